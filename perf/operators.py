@@ -170,7 +170,6 @@ def prepare(case, seed):
             seg=torch.as_tensor(seg).to(DEVICE),
             grad_weight=torch.randn((T, k), generator=gen, device=DEVICE) * unit,
             grad_loss=torch.rand(S, generator=gen, device=DEVICE) * (unit * T / S),
-            stat=torch.zeros(T, device=DEVICE),
             counts=torch.zeros((S, E), dtype=torch.int32, device=DEVICE),
             routed=torch.zeros(S, dtype=torch.int32, device=DEVICE),
             prob_sum=torch.zeros((S, E), device=DEVICE),
@@ -196,17 +195,17 @@ def _own_run(st):
         B.nimble_moe_route(st["x"], st["index"], st["weight"], d_bias=st["bias"], **form)
         return dict(index=st["index"], weight=st["weight"])
     sums = dict(d_counts=st["counts"], d_routed=st["routed"])
-    B.nimble_moe_route(st["x"], st["index"], st["weight"], d_bias=st["bias"], d_stat=st["stat"],
+    B.nimble_moe_route(st["x"], st["index"], st["weight"], d_bias=st["bias"],
                        d_prob_sum=st["prob_sum"], d_seg_ptr=st["seg"], **sums, **form)
     B.nimble_moe_balance_loss(st["counts"], st["routed"], st["prob_sum"], case["top_k"], ALPHA,
                               st["loss"])
-    B.nimble_moe_route_backward(st["x"], st["index"], st["weight"], st["stat"], st["grad_logits"],
+    B.nimble_moe_route_backward(st["x"], st["index"], st["weight"], st["grad_logits"],
                                 d_grad_weight=st["grad_weight"], alpha=ALPHA,
                                 d_grad_loss=st["grad_loss"], d_seg_ptr=st["seg"], **sums, **form)
     return {n: st[n] for n in _TRAINED}
 
 
-_TRAINED = ("index", "weight", "stat", "counts", "routed", "prob_sum", "loss", "grad_logits")
+_TRAINED = ("index", "weight", "counts", "routed", "prob_sum", "loss", "grad_logits")
 
 
 # ---- the plain form -------------------------------------------------------------------------
@@ -287,7 +286,7 @@ def _plain_run(st):
         dx = prob * torch.sigmoid(-x) * (c - rest)
         a = a * torch.sigmoid(-torch.gather(x, 1, idx.clamp(min=0)))
     dx.scatter_add_(1, idx.clamp(min=0), torch.where(have, a, 0.0))
-    return dict(out, stat=stat, counts=counts.int(), routed=routed.int(),
+    return dict(out, counts=counts.int(), routed=routed.int(),
                 prob_sum=prob_sum.float(), loss=loss.float(), grad_logits=dx.to(st["x"].dtype))
 
 
@@ -362,7 +361,7 @@ def exact(case, seed):
     f = {n: st[n].double().cpu().numpy() for n in ("grad_weight", "grad_loss") if n in st}
     out = dict(index=np.full((T, k), -1, dtype=np.int32), weight=np.zeros((T, k)))
     if train:
-        out.update(stat=np.zeros(T), counts=np.zeros((S, E), dtype=np.int32),
+        out.update(counts=np.zeros((S, E), dtype=np.int32),
                    routed=np.zeros(S, dtype=np.int32), prob_sum=np.zeros((S, E)),
                    loss=np.zeros(S), grad_logits=np.zeros((T, E)))
     for s in range(S):
@@ -392,7 +391,6 @@ def exact(case, seed):
         out["weight"][rows] = w
         if not train:
             continue
-        out["stat"][rows] = total[:, 0]
         cnt = np.bincount(pick[there], minlength=E)
         out["counts"][s], out["routed"][s], out["prob_sum"][s] = cnt, len(rows), p.sum(0)
         unit = ALPHA * E / k / len(rows) ** 2
@@ -424,6 +422,6 @@ def work(case):
     size = T * E * z + T * k * 8 + (E * 4 if case["bias"] else 0) + (T if case["padded"] else 0)
     ops = T * (5 * E + 4 * k)
     if case["op"] == "train":
-        size += T * E * z + T * k * 4 + T * 4 + S * (E * 8 + 16)
+        size += T * E * z + T * k * 4 + S * (E * 8 + 16)
         ops += T * (8 * E + 6 * k)
     return dict(bytes=size, flops=ops)
