@@ -5,3 +5,4 @@ Nothing in the product path (`paper_2604_00317_amd`) may import this package; on
 """
 from .oracle import solve, alg1, solve_adaptive, chunked_sum, build, max_threads, set_threads, congestion  # noqa: F401
 from .quantize_oracle import quantize  # noqa: F401
+from . import moe_oracle as moe  # noqa: F401

@@ -1,6 +1,6 @@
 """ctypes binding of libnimble_plan.so: argument marshalling only.
 
-The functions carry the names of the C ABI (include/nimble_plan.h, and
+The functions carry the names of the C ABI (include/nimble_plan.h, include/nimble_moe.h, and
 include/nimble_plan_debug.h for the test and benchmark helpers).  Device buffers are torch
 tensors (torch is used for device memory and streams, nothing else); every step of a plan runs
 in the library's HIP kernels.  If the library is missing this module raises -- there is no
@@ -19,6 +19,9 @@ LIB_PATH = os.path.join(_HERE, "libnimble_plan.so")
 
 NIMBLE_OK, NIMBLE_ERR_INVALID, NIMBLE_ERR_ALLOC, NIMBLE_ERR_HIP, NIMBLE_ERR_RANGE = range(5)
 NIMBLE_COST_SUM, NIMBLE_COST_MAX, NIMBLE_LAYOUT_BATCH = 0, 1, 2
+NIMBLE_F32, NIMBLE_F16, NIMBLE_BF16 = range(3)
+NIMBLE_MOE_SIGMOID, NIMBLE_MOE_RENORM = 1, 2
+NIMBLE_MOE_WAY_BACK = 1
 NIMBLE_REGIME_AUTO, NIMBLE_REGIME_RESIDENT, NIMBLE_REGIME_STREAM, NIMBLE_REGIME_PERSISTENT = \
     range(4)
 
@@ -41,6 +44,9 @@ EXPORTS = [
     "nimble_debug_patches_gave_up",
     "nimble_debug_refuse_cooperative", "nimble_debug_fail_patch_build",
     "nimble_topo_last_patches", "nimble_topo_alg1_form",
+    "nimble_moe_route", "nimble_moe_route_scratch_bytes", "nimble_moe_balance_loss",
+    "nimble_moe_route_backward", "nimble_moe_counts", "nimble_moe_counts_scratch_bytes",
+    "nimble_moe_traffic",
 ]
 
 _lib = None
@@ -148,6 +154,23 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.nimble_host_patch_check.argtypes = [i32, i32, vp, i32, vp, vp, i32, i32, vp]
     lib.nimble_host_layout_stats.restype = ctypes.c_int
     lib.nimble_host_layout_stats.argtypes = [i32, i32, vp, i32, vp, vp, vp]
+    flt = ctypes.c_float
+    lib.nimble_moe_route.restype = ctypes.c_int
+    lib.nimble_moe_route.argtypes = [i32, i32, i32, u32, i32, vp, i64, vp, vp, flt, i32, vp, vp, vp,
+                                     vp, vp, vp, vp, i64, vp]
+    lib.nimble_moe_route_scratch_bytes.restype = i64
+    lib.nimble_moe_route_scratch_bytes.argtypes = [i32, i32, i32]
+    lib.nimble_moe_balance_loss.restype = ctypes.c_int
+    lib.nimble_moe_balance_loss.argtypes = [i32, i32, i32, vp, vp, vp, flt, vp, vp]
+    lib.nimble_moe_route_backward.restype = ctypes.c_int
+    lib.nimble_moe_route_backward.argtypes = [i32, i32, i32, u32, i32, vp, i64, vp, flt, i32, vp, vp,
+                                              vp, vp, flt, vp, vp, vp, vp, i64, vp]
+    lib.nimble_moe_counts.restype = ctypes.c_int
+    lib.nimble_moe_counts.argtypes = [i32, i32, vp, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp]
+    lib.nimble_moe_counts_scratch_bytes.restype = i64
+    lib.nimble_moe_counts_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.nimble_moe_traffic.restype = ctypes.c_int
+    lib.nimble_moe_traffic.argtypes = [i32, i32, vp, dbl, i32, vp, vp, u32, vp, vp]
     for name in ("nimble_host_build_reverse", "nimble_host_build_reverse_streaming"):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = [i32, i32, vp, i32, vp, vp, vp, vp, vp]
@@ -352,6 +375,212 @@ def nimble_plan_quantize(topo: Topo, d_traffic, d_splits, iters: int, chi: int,
         _dev_ptr(d_splits, "float64", topo.n_paths, "d_splits"), int(iters), int(chi),
         float(small_threshold), _dev_ptr(d_flows, "float64", topo.n_paths, "d_flows"),
         _stream_ptr(stream)))
+
+
+# ---- routing (include/nimble_moe.h) -----------------------------------------------------------
+
+class _Call:
+    """The GPU and the stream of a call: every tensor is on the GPU of the first one, which is made
+    current for the call.  A stream of None is the current one of that GPU."""
+
+    def __init__(self, first, stream):
+        import torch
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise TypeError("routing operators take device tensors")
+        self.device = first.device
+        self.given = stream
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        elif stream.device != self.device:
+            raise ValueError("the stream is on another device than the tensors")
+        self.stream = stream.cuda_stream
+
+    def ptr(self, t, dtype, shape, what):
+        """Pointer of a contiguous tensor of that shape; None stays None."""
+        if t is None:
+            return None
+        if t.device != self.device:
+            raise ValueError(f"{what} must be on {self.device}")
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {dtype} of shape {shape}")
+        return t.data_ptr()
+
+    def matrix(self, t, dtype, shape, what):
+        """Pointer and row stride of a matrix whose rows are contiguous."""
+        if t.device != self.device:
+            raise ValueError(f"{what} must be on {self.device}")
+        if t.dtype != dtype or tuple(t.shape) != shape or \
+                (shape[0] > 0 and shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} must be {dtype} of shape {shape} with contiguous rows")
+        stride = t.stride(0) if shape[0] > 1 else shape[1]
+        if stride < shape[1]:
+            raise ValueError(f"rows of {what} must not overlap")
+        return t.data_ptr(), stride
+
+    def scratch(self, t, nbytes):
+        """(pointer, bytes, owner) of scratch memory: the tensor given, or memory of the call's own
+        stream, which torch hands out again only behind the call's work."""
+        import torch
+        if nbytes < 0:
+            return None, 0, None             # sizes the library refuses: it says why
+        if t is None:
+            if self.given is None:
+                t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            else:
+                with torch.cuda.stream(self.given):
+                    t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        elif t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"d_scratch must be contiguous and on {self.device}")
+        return t.data_ptr(), t.numel() * t.element_size(), t
+
+    def run(self, fn, *args):
+        import torch
+        if torch.cuda.current_device() == self.device.index:
+            _check(fn(*args, self.stream))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*args, self.stream))
+
+
+def _moe_dtype(t):
+    import torch
+    kinds = {torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16, torch.bfloat16: NIMBLE_BF16}
+    if t.dtype not in kinds:
+        raise ValueError("d_logits must be float32, float16 or bfloat16")
+    if t.dim() != 2:
+        raise ValueError("d_logits must be [tokens][experts]")
+    return kinds[t.dtype]
+
+
+def _moe_flags(sigmoid: bool, renorm: bool) -> int:
+    return (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0)
+
+
+def _moe_segments(d_seg_ptr) -> int:
+    return 1 if d_seg_ptr is None else d_seg_ptr.numel() - 1
+
+
+def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, renorm: bool = True,
+                     scale: float = 1.0, d_bias=None, d_keep=None, d_seg_ptr=None,
+                     d_counts=None, d_routed=None, d_prob_sum=None, d_scratch=None,
+                     stream=None) -> None:
+    """Chooses d_index.shape[1] experts per row of d_logits [tokens][experts] (float32, float16 or
+    bfloat16; rows may be strided), with their weights.  d_counts [segments][experts], d_routed
+    [segments] and d_prob_sum [segments][experts] are wanted together or not at all."""
+    import torch
+    lib = load_library()
+    kind = _moe_dtype(d_logits)
+    c = _Call(d_logits, stream)
+    tokens, experts = d_logits.shape
+    top_k = d_index.shape[1] if d_index.dim() == 2 else 0
+    n_seg = _moe_segments(d_seg_ptr)
+    x, stride = c.matrix(d_logits, d_logits.dtype, (tokens, experts), "d_logits")
+    scratch = nbytes = owner = None
+    if d_counts is not None:
+        scratch, nbytes, owner = c.scratch(
+            d_scratch, lib.nimble_moe_route_scratch_bytes(tokens, experts, n_seg))
+    c.run(lib.nimble_moe_route, tokens, experts, top_k, _moe_flags(sigmoid, renorm), kind, x, stride,
+          c.ptr(d_bias, torch.float32, (experts,), "d_bias"),
+          c.ptr(d_keep, torch.uint8, (tokens,), "d_keep"), scale, n_seg,
+          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
+          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"),
+          c.ptr(d_weight, torch.float32, (tokens, top_k), "d_weight"),
+          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
+          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
+          c.ptr(d_prob_sum, torch.float32, (n_seg, experts), "d_prob_sum"), scratch, nbytes or 0)
+
+
+def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 1) -> int:
+    return int(load_library().nimble_moe_route_scratch_bytes(tokens, experts, n_segments))
+
+
+def nimble_moe_balance_loss(d_counts, d_routed, d_prob_sum, top_k: int, alpha: float, d_loss,
+                            stream=None) -> None:
+    """d_loss [segments] from the sums nimble_moe_route gives."""
+    import torch
+    c = _Call(d_counts, stream)
+    if d_counts.dim() != 2:
+        raise ValueError("d_counts must be [segments][experts]")
+    n_seg, experts = d_counts.shape
+    c.run(load_library().nimble_moe_balance_loss, n_seg, experts, top_k,
+          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
+          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
+          c.ptr(d_prob_sum, torch.float32, (n_seg, experts), "d_prob_sum"), alpha,
+          c.ptr(d_loss, torch.float32, (n_seg,), "d_loss"))
+
+
+def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *,
+                              sigmoid: bool = False, renorm: bool = True, scale: float = 1.0,
+                              d_keep=None, d_seg_ptr=None, d_grad_weight=None, alpha: float = 0.0,
+                              d_counts=None, d_routed=None, d_grad_loss=None,
+                              stream=None) -> None:
+    """Gradient of the logits from those of weights and loss, with the flags, scale, d_keep and
+    segments of the call of nimble_moe_route that gave d_index and d_weight."""
+    import torch
+    kind = _moe_dtype(d_logits)
+    c = _Call(d_logits, stream)
+    tokens, experts = d_logits.shape
+    top_k = d_index.shape[1] if d_index.dim() == 2 else 0
+    n_seg = _moe_segments(d_seg_ptr)
+    x, stride = c.matrix(d_logits, d_logits.dtype, (tokens, experts), "d_logits")
+    dx, grad_stride = c.matrix(d_grad_logits, d_logits.dtype, (tokens, experts), "d_grad_logits")
+    c.run(load_library().nimble_moe_route_backward, tokens, experts, top_k,
+          _moe_flags(sigmoid, renorm), kind, x, stride,
+          c.ptr(d_keep, torch.uint8, (tokens,), "d_keep"), scale, n_seg,
+          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
+          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"),
+          c.ptr(d_weight, torch.float32, (tokens, top_k), "d_weight"),
+          c.ptr(d_grad_weight, torch.float32, (tokens, top_k), "d_grad_weight"), alpha,
+          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
+          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
+          c.ptr(d_grad_loss, torch.float32, (n_seg,), "d_grad_loss"), dx, grad_stride)
+
+
+def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=None,
+                      d_rank_tokens=None, d_seg_ptr=None, d_scratch=None, stream=None) -> None:
+    """Slots per expert (d_counts [segments][experts]) and distinct tokens per destination GPU
+    (d_rank_tokens [segments][ranks], by d_expert_rank [experts]) of routed tokens."""
+    import torch
+    lib = load_library()
+    c = _Call(d_index, stream)
+    if d_index.dim() != 2:
+        raise ValueError("d_index must be [tokens][top_k]")
+    tokens, top_k = d_index.shape
+    n_seg = _moe_segments(d_seg_ptr)
+    ranks = 0 if d_rank_tokens is None else d_rank_tokens.shape[-1]
+    scratch, nbytes, owner = c.scratch(
+        d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg))
+    c.run(lib.nimble_moe_counts, tokens, top_k,
+          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"), experts, n_seg,
+          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
+          c.ptr(d_expert_rank, torch.int32, (experts,), "d_expert_rank"), ranks,
+          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
+          c.ptr(d_rank_tokens, torch.int32, (n_seg, ranks), "d_rank_tokens"), scratch, nbytes)
+
+
+def nimble_moe_counts_scratch_bytes(tokens: int, top_k: int, experts: int, n_ranks: int = 0,
+                                    n_segments: int = 1) -> int:
+    return int(load_library().nimble_moe_counts_scratch_bytes(tokens, top_k, experts, n_ranks,
+                                                              n_segments))
+
+
+def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traffic, *, d_src=None,
+                       d_dst=None, way_back: bool = False, stream=None) -> None:
+    """Demand vectors d_traffic [batch][n_comm] of d_rank_tokens, [batch][ranks][ranks] or the
+    [batch * ranks][ranks] that nimble_moe_counts fills with a segment per source GPU."""
+    import torch
+    c = _Call(d_rank_tokens, stream)
+    ranks = d_rank_tokens.shape[-1]
+    if d_rank_tokens.numel() != batch * ranks * ranks:
+        raise ValueError("d_rank_tokens must be [batch][ranks][ranks]")
+    if batch < 1 or d_traffic.numel() % batch:
+        raise ValueError("d_traffic must be [batch][commodities]")
+    n_comm = d_traffic.numel() // batch
+    c.run(load_library().nimble_moe_traffic, batch, ranks,
+          c.ptr(d_rank_tokens, torch.int32, tuple(d_rank_tokens.shape), "d_rank_tokens"),
+          bytes_per_token, n_comm, c.ptr(d_src, torch.int32, (n_comm,), "d_src"),
+          c.ptr(d_dst, torch.int32, (n_comm,), "d_dst"), NIMBLE_MOE_WAY_BACK if way_back else 0,
+          c.ptr(d_traffic, torch.float64, tuple(d_traffic.shape), "d_traffic"))
 
 
 def nimble_debug_run_phase(topo: Topo, phase: int, reps: int, d_traffic, stream=None) -> None:
@@ -572,3 +801,32 @@ def plan_alg1(topo: Topo, traffic, phi: float, chi: float, max_sweeps: int = 1 <
     if single:
         return f[0], float(lam.item()), int(sweeps.item())
     return f, lam.cpu().numpy(), sweeps.cpu().numpy()
+
+
+def plan_routed(topo: Topo, d_logits, d_seg_ptr, d_expert_rank, top_k: int, bytes_per_token: float,
+                eps: float, iters: int, *, sigmoid: bool = False, d_bias=None, d_src=None,
+                d_dst=None):
+    """Convenience wrapper of the routing operators and the planner: logits [tokens][experts] of all
+    source GPUs (one segment each, d_seg_ptr [ranks + 1]) in; a dict of device tensors out: the
+    choice (index, weight), rank_tokens, the demand (traffic), splits and lambda of its plan.  Only
+    enqueues work on the current stream.  d_src and d_dst: the GPUs of the commodities, where they
+    are not all ordered pairs in row-major order."""
+    import torch
+    dev = d_logits.device
+    tokens, experts = d_logits.shape
+    ranks = d_seg_ptr.numel() - 1
+    with torch.cuda.device(dev):
+        out = dict(index=torch.full((tokens, top_k), -1, dtype=torch.int32, device=dev),
+                   weight=torch.zeros((tokens, top_k), dtype=torch.float32, device=dev),
+                   rank_tokens=torch.empty((ranks, ranks), dtype=torch.int32, device=dev),
+                   traffic=torch.empty(topo.n_comm, dtype=torch.float64, device=dev),
+                   splits=torch.empty(topo.n_paths, dtype=torch.float64, device=dev),
+                   lam=torch.empty(1, dtype=torch.float64, device=dev))
+        nimble_moe_route(d_logits, out["index"], out["weight"], sigmoid=sigmoid, d_bias=d_bias,
+                         d_seg_ptr=d_seg_ptr)
+        nimble_moe_counts(out["index"], experts, d_expert_rank=d_expert_rank,
+                          d_rank_tokens=out["rank_tokens"], d_seg_ptr=d_seg_ptr)
+        nimble_moe_traffic(1, out["rank_tokens"], bytes_per_token, out["traffic"], d_src=d_src,
+                           d_dst=d_dst)
+        nimble_plan_solve(topo, out["traffic"], eps, iters, out["splits"], out["lam"])
+    return out

@@ -22,6 +22,7 @@
 #include "../../include/nimble_plan_debug.h"
 #include "host_topo.hpp"
 #include "kernels.hpp"
+#include "report.hpp"
 
 #ifndef NIMBLE_STATIC_SCRATCH_BYTES
 #define NIMBLE_STATIC_SCRATCH_BYTES (32u << 20)
@@ -105,6 +106,33 @@ hipError_t static_scratch_of(int device, unsigned char **out)
 }
 
 }  // namespace
+
+namespace nimble {
+
+void report_clear() noexcept { g_last_error.clear(); }
+
+// (a message that finds no memory is left out: the status says enough)
+nimble_status_t report(nimble_status_t status, const char *message) noexcept
+{
+    try {
+        g_last_error = message;
+    } catch (...) {
+        g_last_error.clear();
+    }
+    return status;
+}
+
+nimble_status_t report_hip(hipError_t e, const char *what) noexcept
+{
+    try {
+        return fail_hip(e, what);
+    } catch (...) {
+        g_last_error.clear();
+        return NIMBLE_ERR_HIP;
+    }
+}
+
+}  // namespace nimble
 
 struct nimble_topo {
     nimble::DeviceTopo d{};

@@ -1,0 +1,530 @@
+"""The routing operators against oracle/moe_oracle.py, through the C ABI.
+
+Indices, counts and demands have to be equal.  Bounds of computed numbers are rounding counts, U =
+2^-24 a binary32 rounding.  A probability or weight is exp(x - m) over a sum: the argument's product
+with log2(e) is off by 1.5 U |x - m| (constant and product) and |x - m| U (difference), which the exp
+makes relative; exp2, division and products add a few U, a sum of E terms over lanes E/64 + 6.  `rel` below has these with a
+factor of one and a half or more.  A gradient is a sum of products whose magnitudes the oracle
+returns: three such factors on them, and half a step of its type.  Results below 2^-126 may be 0.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from oracle import moe_oracle as M
+from paper_2604_00317_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TINY = 2.0 ** -125
+HALF_STEP = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+SMALLEST = {"float32": 0.0, "float16": 2.0 ** -25, "bfloat16": 0.0}   # half a step at zero
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2604_00317_amd import binding
+    binding.load_library(build_if_missing=False)
+    return binding
+
+
+def rel(x):
+    """Relative bound of the probabilities of every row of x."""
+    with np.errstate(invalid="ignore"):
+        fine = np.where(np.isfinite(x), x, np.nan)
+    top = np.nanmax(np.where(np.isnan(fine), -1e30, fine), axis=1)
+    low = np.nanmin(np.where(np.isnan(fine), 1e30, fine), axis=1)
+    spread = np.clip(top - low, 0, 100)
+    size = np.clip(np.abs(top), 0, 100)               # a sigmoid's own argument
+    return (4 * spread + 4 * size + x.shape[1] / 32 + 64) * U
+
+
+def run(B, x, top_k, sigmoid=False, renorm=True, scale=1.0, bias=None, keep=None, seg=None, sums=True,
+        grad_weight=None, alpha=0.0, grad_loss=None, backward=False, stream=None, grad_out=None):
+    """Everything a training step gives, as numpy; outputs start at -2 / NaN."""
+    import torch
+    T, E = x.shape
+    dev = x.device
+    S = 1 if seg is None else len(seg) - 1
+    d = lambda a, t: None if a is None else torch.as_tensor(np.asarray(a)).to(dev, t)   # noqa: E731
+    o = dict(index=torch.full((T, top_k), -2, dtype=torch.int32, device=dev),
+             weight=torch.full((T, top_k), math.nan, device=dev))
+    form = dict(sigmoid=sigmoid, renorm=renorm, scale=scale, d_keep=d(keep, torch.uint8),
+                d_seg_ptr=d(seg, torch.int32), stream=stream)
+    kw = {}
+    if sums:
+        o.update(counts=torch.full((S, E), -7, dtype=torch.int32, device=dev),
+                 routed=torch.full((S,), -7, dtype=torch.int32, device=dev),
+                 prob_sum=torch.full((S, E), math.nan, device=dev))
+        kw = dict(d_counts=o["counts"], d_routed=o["routed"], d_prob_sum=o["prob_sum"])
+    B.nimble_moe_route(x, o["index"], o["weight"], d_bias=d(bias, torch.float32), **kw, **form)
+    if sums:
+        o["loss"] = torch.full((S,), math.nan, device=dev)
+        B.nimble_moe_balance_loss(o["counts"], o["routed"], o["prob_sum"], top_k, alpha, o["loss"], stream=stream)
+    if backward:
+        o["grad"] = torch.full((T, E), math.nan, dtype=x.dtype, device=dev) if grad_out is None else grad_out
+        loss = dict(d_counts=o["counts"], d_routed=o["routed"], d_grad_loss=d(grad_loss, torch.float32))
+        B.nimble_moe_route_backward(x, o["index"], o["weight"], o["grad"], alpha=alpha,
+                                    d_grad_weight=d(grad_weight, torch.float32),
+                                    **(loss if grad_loss is not None else {}), **form)
+    torch.cuda.synchronize()
+    return {n: t.float().cpu().numpy() if t.dtype.is_floating_point else t.cpu().numpy() for n, t in o.items()}
+
+
+def check(got, x, top_k, dtype="float32", **kw):
+    """Against the oracle on x, the float32 values of the logits."""
+    sigmoid, renorm, scale = kw.get("sigmoid", False), kw.get("renorm", True), kw.get("scale", 1.0)
+    bias = kw.get("bias")
+    bias = None if bias is None else np.asarray(bias, dtype=np.float32)
+    keep, ends = kw.get("keep"), kw.get("seg")
+    ref = M.route(x, top_k, sigmoid, renorm, scale, bias, keep, ends)
+    r = rel(x)
+    assert np.array_equal(got["index"], ref["index"])
+    np.testing.assert_array_equal(np.isnan(got["weight"]), np.isnan(ref["weight"]))
+    ok = ~np.isnan(ref["weight"])
+    bound = (r[:, None] * np.abs(np.nan_to_num(ref["weight"])) + TINY)
+    assert (np.abs(got["weight"] - ref["weight"])[ok] <= bound[ok]).all()
+    if "counts" in got:
+        assert np.array_equal(got["counts"], ref["counts"])
+        assert np.array_equal(got["routed"], ref["routed"])
+        np.testing.assert_array_equal(np.isnan(got["prob_sum"]), np.isnan(ref["prob_sum"]))
+        for s in range(got["counts"].shape[0]):
+            a, b = (0, x.shape[0]) if ends is None else (ends[s], ends[s + 1])
+            if a < b and not np.isnan(ref["prob_sum"][s]).any():
+                bound = (r[a:b, None] * ref["prob"][a:b]).sum(0) + (b - a + 16) * U * ref["prob_sum"][s] + TINY * (b - a)
+                assert (np.abs(got["prob_sum"][s] - ref["prob_sum"][s]) <= bound).all()
+        loss = M.balance_loss(ref["counts"], ref["routed"], got["prob_sum"], top_k,
+                               float(np.float32(kw.get("alpha", 0.0))))
+        np.testing.assert_allclose(got["loss"], loss, rtol=2 * U, atol=TINY)
+    if "grad" in got:
+        gw, gl = kw.get("grad_weight"), kw.get("grad_loss")
+        dx, mag = M.route_backward(x, got["index"], got["weight"].astype(np.float64), sigmoid, renorm, float(np.float32(scale)), keep, ends, gw,
+                                   float(np.float32(kw.get("alpha", 0.0))),
+                                   ref["counts"] if gl is not None else None, ref["routed"], gl)
+        np.testing.assert_array_equal(np.isnan(got["grad"]), np.isnan(dx))
+        fine = ~np.isnan(dx)
+        b = 3 * rel(x)[:, None] * np.nan_to_num(mag)
+        bound = b + HALF_STEP[dtype] * (np.abs(np.nan_to_num(dx)) + b) + SMALLEST[dtype] + TINY
+        assert (np.abs(got["grad"] - dx)[fine] <= bound[fine]).all()
+    return ref
+
+
+def logits(rng, T, E, dtype, spread=2.0):
+    import torch
+    x = torch.as_tensor(rng.normal(size=(T, E)) * spread).to("cuda:0", getattr(torch, dtype))
+    return x
+
+
+@pytest.mark.parametrize("E", [1, 2, 7, 8, 60, 63, 64, 65, 96, 128, 130, 160, 255, 256, 257, 384, 512, 1000,
+                               1024, 1025, 2047, 2048])
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_every_width_and_type(B, E, dtype):
+    rng = np.random.default_rng(E)
+    T, k = (67 if E <= 512 else 19), min(E, 8)
+    x = logits(rng, T, E, dtype)
+    bias = rng.normal(size=E)
+    keep = rng.random(T) < 0.8
+    form = dict(keep=keep, seg=[0, T // 3, T // 3, T - 2], grad_weight=rng.normal(size=(T, k)).astype(np.float32),
+                grad_loss=rng.normal(size=3).astype(np.float32), alpha=0.3, scale=2.5)
+    for sigmoid in (False, True):
+        for renorm in (False, True):
+            kw = dict(form, sigmoid=sigmoid, renorm=renorm, bias=bias if renorm else None)
+            print(f"[moe] E={E} {dtype} sigmoid={sigmoid} renorm={renorm}", flush=True)
+            got = run(B, x, k, backward=True, **kw)
+            check(got, x.float().cpu().numpy(), k, dtype, **kw)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 5, 9, 15, 16])
+@pytest.mark.parametrize("E", [16, 100, 700])
+def test_every_top_k_with_ties(B, k, E):
+    """Logits of five values, zeros of both signs among them: nearly every choice is a tie."""
+    import torch
+    rng = np.random.default_rng(k * E)
+    v = np.array([-1.0, -0.0, 0.0, 0.5, 2.0], dtype=np.float32)
+    x = v[rng.integers(0, 5, (33, E))]
+    x[5] = -0.0
+    x[6] = 1.0
+    got = run(B, torch.as_tensor(x).to("cuda:0"), k, renorm=False)
+    check(got, x, k, renorm=False)
+    got = run(B, torch.as_tensor(x).to("cuda:0", torch.bfloat16), k, bias=v[rng.integers(0, 5, E)], sums=False)
+    assert set(got) == {"index", "weight"}
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E", [5, 64, 200, 1024])
+def test_rows_at_the_edges(B, dtype, sigmoid, E):
+    """Masked experts and rows, one expert left, lowest and largest values, NaN and infinities; rows
+    that are left out hold NaN."""
+    import torch
+    rng = np.random.default_rng(3)
+    T, k = 24, 4
+    t = getattr(torch, dtype)
+    low, high = torch.finfo(t).min, torch.finfo(t).max
+    x = rng.normal(size=(T, E))
+    x[0] = -np.inf
+    x[1, 1:] = -np.inf
+    x[2] = low
+    x[3, : E // 2] = low
+    x[4] = high
+    x[5, 2] = high
+    x[6] = -300.0 + x[6]
+    x[7] = 300.0 + x[7]
+    x[8, E - 1] = np.nan
+    x[9, 0] = np.inf
+    x[10] = np.nan
+    x[11] = np.inf
+    x[12, : E - 2] = -np.inf
+    x[13, 3] = -np.inf
+    x[14, 0], x[14, 1] = -np.inf, np.nan
+    x[15] = 0.0
+    x = torch.as_tensor(x).to("cuda:0", t)
+    keep = np.ones(T, dtype=np.uint8)
+    keep[10] = keep[20] = 0
+    seg = [0, 4, 8, 16, 16, 24]                       # NaN rows are in the third, padding in two
+    f = dict(sigmoid=sigmoid, keep=keep, seg=seg, grad_weight=rng.normal(size=(T, k)).astype(np.float32),
+             grad_loss=rng.normal(size=5).astype(np.float32), alpha=0.5)
+    for renorm in (False, True):
+        got = run(B, x, k, backward=True, renorm=renorm, **f)
+        ref = check(got, x.float().cpu().numpy(), k, dtype, renorm=renorm, **f)
+        assert ref["index"][0].max() == -1 and ref["index"][1].tolist()[1:] == [-1] * 3
+        assert not got["grad"][0].any() and not got["grad"][10].any() and not got["grad"][20].any()
+
+
+def test_a_bias_that_excludes_and_one_that_forces(B):
+    import torch
+    rng = np.random.default_rng(9)
+    x = rng.normal(size=(9, 40)).astype(np.float32)
+    x[2, 7] = -np.inf
+    bias = np.zeros(40, dtype=np.float32)
+    bias[3], bias[4], bias[7], bias[11] = -np.inf, np.nan, np.inf, np.inf
+    kw = dict(bias=bias, grad_weight=rng.normal(size=(9, 5)).astype(np.float32),
+              grad_loss=np.ones(1, dtype=np.float32), alpha=1.0, renorm=False)
+    got = run(B, torch.as_tensor(x).to("cuda:0"), 5, backward=True, **kw)
+    check(got, x, 5, **kw)
+    assert not np.isin(got["index"], [3, 4]).any() and 7 not in got["index"][2] and (got["index"][:, 0] >= 7).all()
+    all_off = np.full(40, -np.inf, dtype=np.float32)
+    kw["bias"] = all_off
+    got = run(B, torch.as_tensor(x).to("cuda:0"), 5, backward=True, **kw)
+    check(got, x, 5, **kw)
+    assert (got["index"] == -1).all() and not got["grad"].any() and not got["counts"].any()
+
+
+@pytest.mark.parametrize("E,pad,shift", [(64, 0, 1), (64, 3, 0), (160, 4, 4), (256, 8, 2), (500, 12, 0), (1024, 1, 1)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_strided_and_unaligned_rows(B, E, pad, shift, dtype):
+    import torch
+    rng = np.random.default_rng(E + pad)
+    T, k = 21, 6
+    buf = torch.full((T * (E + pad) + 16,), math.nan, dtype=getattr(torch, dtype), device="cuda:0")
+    x = buf[shift:shift + T * (E + pad)].view(T, E + pad)[:, :E]
+    x.copy_(torch.as_tensor(rng.normal(size=(T, E))))
+    out = torch.full((T * (E + pad) + 16,), 77.0, dtype=buf.dtype, device="cuda:0")
+    g = out[shift:shift + T * (E + pad)].view(T, E + pad)[:, :E]
+    kw = dict(grad_weight=rng.normal(size=(T, k)).astype(np.float32), grad_loss=np.ones(1, dtype=np.float32),
+              alpha=0.25, renorm=False)
+    got = run(B, x, k, backward=True, grad_out=g, **kw)
+    check(got, x.float().cpu().numpy(), k, dtype, **kw)
+    g.fill_(77.0)
+    assert (out == 77.0).all()                        # nothing between the rows was written
+
+
+@pytest.mark.parametrize("T", [0, 1, 2, 7, 8, 9, 500, 1023, 8191, 8200])
+@pytest.mark.parametrize("S", [1, 3, 40])
+def test_row_counts_and_segments(B, T, S):
+    """Segments of any length, empty ones at the ends and in between, rows before the first and behind the
+    last, which stay as they were."""
+    import torch
+    rng = np.random.default_rng(T + S)
+    E, k = 24, 3
+    seg = np.sort(rng.integers(0, T + 1, S + 1)).astype(np.int32)
+    seg[S // 2:S // 2 + 2] = seg[S // 2]
+    x = logits(rng, T, E, "float32")
+    kw = dict(seg=seg, grad_weight=rng.normal(size=(T, k)).astype(np.float32),
+              grad_loss=rng.normal(size=S).astype(np.float32), alpha=0.25)
+    got = run(B, x, k, backward=True, **kw)
+    if T:
+        check(got, x.cpu().numpy(), k, **kw)
+    else:
+        assert not got["counts"].any() and not got["routed"].any() and not got["prob_sum"].any()
+        assert not got["loss"].any()
+    served = run(B, x, k, seg=seg, sums=False)
+    assert np.array_equal(served["index"], got["index"])
+    assert np.array_equal(served["weight"], got["weight"], equal_nan=True)
+
+
+def test_offsets_out_of_range_are_cut(B):
+    rng = np.random.default_rng(1)
+    x = logits(rng, 20, 16, "float32")
+    a = run(B, x, 2, seg=[-5, 7, 1 << 30])
+    b = run(B, x, 2, seg=[0, 7, 20])
+    for n in ("index", "counts", "routed", "prob_sum"):
+        assert np.array_equal(a[n], b[n]), n
+
+
+def test_results_are_the_same_on_every_run(B):
+    rng = np.random.default_rng(8)
+    x = logits(rng, 5000, 256, "bfloat16")
+    kw = dict(seg=[0, 1000, 1001, 4999], grad_weight=rng.normal(size=(5000, 8)).astype(np.float32),
+              grad_loss=np.ones(3, dtype=np.float32), alpha=0.1, backward=True)
+    a = run(B, x, 8, **kw)
+    for _ in range(3):
+        b = run(B, x, 8, **kw)
+        assert all(np.array_equal(a[n], b[n], equal_nan=True) for n in a)
+
+
+def test_parts_of_the_gradient_that_are_left_out(B):
+    rng = np.random.default_rng(12)
+    x = logits(rng, 30, 100, "float32")
+    gw, gl = rng.normal(size=(30, 4)).astype(np.float32), np.ones(1, dtype=np.float32)
+    for sigmoid in (False, True):
+        for renorm in (False, True):
+            for kw in (dict(grad_weight=gw), dict(grad_loss=gl, alpha=0.5), dict()):
+                kw.update(sigmoid=sigmoid, renorm=renorm)
+                got = run(B, x, 4, backward=True, **kw)
+                check(got, x.cpu().numpy(), 4, **kw)
+
+
+def test_indices_of_another_router(B):
+    """The gradient takes any indices: the same one twice adds up, those out of range are empty slots."""
+    import torch
+    rng = np.random.default_rng(2)
+    x = rng.normal(size=(6, 70)).astype(np.float32)
+    r = M.route(x, 4, renorm=False)
+    idx = r["index"].copy()
+    idx[0, 1] = idx[0, 0]
+    idx[1, 2], idx[2, 0], idx[3, 3] = 70, -5, 1 << 30
+    d = lambda a: torch.as_tensor(a).to("cuda:0")   # noqa: E731
+    w = rng.random((6, 4)).astype(np.float32)
+    gw = rng.normal(size=(6, 4)).astype(np.float32)
+    out = torch.full((6, 70), math.nan, device="cuda:0")
+    B.nimble_moe_route_backward(d(x), d(idx), d(w), out, renorm=False, d_grad_weight=d(gw))
+    dx, mag = M.route_backward(x, idx, w.astype(np.float64), renorm=False, grad_weight=gw)
+    assert (np.abs(out.cpu().numpy() - dx) <= 3 * rel(x)[:, None] * mag + U * np.abs(dx)).all()
+
+
+def test_offsets_beyond_32_bits(B):
+    """Rows 2^31 + 64 elements apart."""
+    import torch
+    rng = np.random.default_rng(4)
+    T, E, k, stride = 3, 100, 4, (1 << 31) + 64
+    buf = torch.empty(stride * (T - 1) + E, dtype=torch.bfloat16, device="cuda:0")
+    x = buf.as_strided((T, E), (stride, 1))
+    x.copy_(torch.as_tensor(rng.normal(size=(T, E))))
+    out = torch.empty_like(buf).as_strided((T, E), (stride, 1))
+    kw = dict(grad_weight=rng.normal(size=(T, k)).astype(np.float32), grad_loss=np.ones(1, dtype=np.float32),
+              alpha=0.5)
+    got = run(B, x, k, backward=True, grad_out=out, **kw)
+    check(got, x.float().cpu().numpy(), k, "bfloat16", **kw)
+
+
+# ---- counts and demand -----------------------------------------------------------------------
+
+def gpu_counts(B, index, E, seg=None, place=None, ranks=0, counts=True):
+    import torch
+    S = 1 if seg is None else len(seg) - 1
+    d = lambda a: None if a is None else torch.as_tensor(np.asarray(a, dtype=np.int32)).to("cuda:0")   # noqa: E731
+    c = torch.full((S, E), -7, dtype=torch.int32, device="cuda:0") if counts else None
+    r = torch.full((S, ranks), -7, dtype=torch.int32, device="cuda:0") if ranks else None
+    B.nimble_moe_counts(d(index), E, c, d_expert_rank=d(place), d_rank_tokens=r, d_seg_ptr=d(seg))
+    torch.cuda.synchronize()
+    return None if c is None else c.cpu().numpy(), None if r is None else r.cpu().numpy()
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 6, 8, 11, 16])
+@pytest.mark.parametrize("T,E,R,S", [(1, 8, 4, 1), (37, 60, 7, 3), (700, 1024, 512, 5), (3000, 2048, 33, 2),
+                                     (1500, 16, 1, 40), (0, 8, 3, 2)])
+def test_counts(B, k, T, E, R, S):
+    """Any indices: the same expert twice, entries out of range, experts that live nowhere."""
+    rng = np.random.default_rng(k * 1000 + T)
+    index = np.minimum(rng.zipf(1.3, (T, k)) - 1, 1 << 20).astype(np.int32) % (E + 3) - 1
+    place = rng.integers(-1, R + 1, E)
+    seg = np.sort(rng.integers(0, T + 1, S + 1))
+    ref = M.counts(index, E, seg, place, R)
+    c, r = gpu_counts(B, index, E, seg, place, R)
+    assert np.array_equal(c, ref[0]) and np.array_equal(r, ref[1])
+    c, _ = gpu_counts(B, index, E, seg)
+    assert np.array_equal(c, ref[0])
+    _, r = gpu_counts(B, index, E, seg, place, R, counts=False)
+    assert np.array_equal(r, ref[1])
+
+
+def test_counts_of_one_hot_expert(B):
+    T, k = 200001, 3
+    index = np.tile(np.array([5, 9, 2], dtype=np.int32), (T, 1))
+    c, r = gpu_counts(B, index, 12, None, np.arange(12) // 6, 2)
+    assert c[0, 5] == c[0, 9] == c[0, 2] == T and c.sum() == 3 * T and r.tolist() == [[T, T]]
+
+
+@pytest.mark.parametrize("batch,R", [(1, 2), (3, 7), (61, 8), (2, 512)])
+def test_traffic(B, batch, R):
+    import torch
+    rng = np.random.default_rng(R)
+    rt = rng.integers(0, 1 << 20, (batch, R, R)).astype(np.int32)
+    d = torch.as_tensor(rt).to("cuda:0")
+    small = rt if R < 100 else rt[:, :, :]
+    for way_back in (False, True):
+        out = torch.full((batch, R * (R - 1)), math.nan, dtype=torch.float64, device="cuda:0")
+        B.nimble_moe_traffic(batch, d, 14336, out, way_back=way_back)
+        m = small.transpose(0, 2, 1) if way_back else small
+        assert np.array_equal(out.cpu().numpy(), m[:, ~np.eye(R, dtype=bool)] * 14336.0)
+        src, dst = rng.integers(-1, R + 1, 50).astype(np.int32), rng.integers(0, R, 50).astype(np.int32)
+        out = torch.zeros((batch, 50), dtype=torch.float64, device="cuda:0")
+        B.nimble_moe_traffic(batch, d, 0.5, out, way_back=way_back, d_src=torch.as_tensor(src).to("cuda:0"),
+                             d_dst=torch.as_tensor(dst).to("cuda:0"))
+        assert np.array_equal(out.cpu().numpy(), M.traffic(rt, 0.5, src, dst, way_back), equal_nan=True)
+
+
+# ---- together --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cfg", [0, 1])
+def test_from_logits_to_a_plan(B, oracle_mod, cfg):
+    """Router, counts, demand and planner in a row: the plan is that of the oracles in a row."""
+    import torch
+    w = W.make_config(cfg)
+    t = w.topo
+    R = t.meta["n_nodes"] * t.meta["gpus_per_node"]
+    rng = np.random.default_rng(77)
+    E, k, per = 4 * R, 2, 60
+    x = (rng.normal(size=(R * per, E)) - 1.2 * np.log(rng.permutation(E) + 1.0)).astype(np.float32)
+    seg, place = np.arange(R + 1) * per, np.arange(E) // 4
+    ref = M.route(x, k, ends=seg)
+    _, tokens = M.counts(ref["index"], E, seg, place, R)
+    demand = M.traffic(tokens[None], 8192.0)[0]
+    sol = oracle_mod.solve(*t.csr(), demand, w.eps, 50)
+    h = B.nimble_topo_create(*t.csr())
+    try:
+        d = lambda a: torch.as_tensor(np.asarray(a, dtype=np.int32)).to("cuda:0")   # noqa: E731
+        src, dst = (d(t.src), d(t.dst)) if cfg else (None, None)
+        out = B.plan_routed(h, torch.as_tensor(x).to("cuda:0"), d(seg), d(place), k, 8192.0, w.eps, 50,
+                            d_src=src, d_dst=dst)
+        torch.cuda.synchronize()
+    finally:
+        h.close()
+    assert np.array_equal(out["index"].cpu().numpy(), ref["index"])
+    assert np.array_equal(out["traffic"].cpu().numpy(), demand)
+    assert np.array_equal(out["splits"].cpu().numpy(), sol["splits"]) and out["lam"].item() == sol["lam"]
+
+
+def test_captured_steps_replay(B):
+    """Two training steps with the demand, each captured with memory of its own; replayed with new logits,
+    eager work between the replays, and in turn."""
+    import torch
+    dev = "cuda:0"
+    T, E, k, R, S = 777, 160, 6, 5, 5
+    seg = torch.tensor([0, 100, 100, 350, 700, 770], dtype=torch.int32, device=dev)
+    place = (torch.arange(E, dtype=torch.int32, device=dev) // 32)
+    gl = torch.rand(S, device=dev)
+
+    def memory():
+        i, f = dict(dtype=torch.int32, device=dev), dict(device=dev)
+        return dict(x=torch.zeros((T, E), dtype=torch.bfloat16, device=dev), gw=torch.zeros((T, k), **f),
+                    index=torch.full((T, k), -1, **i), weight=torch.zeros((T, k), **f),
+                    counts=torch.zeros((S, E), **i), routed=torch.zeros(S, **i), prob_sum=torch.zeros((S, E), **f),
+                    loss=torch.zeros(S, **f), grad=torch.zeros((T, E), dtype=torch.bfloat16, device=dev),
+                    counts2=torch.zeros((S, E), **i), tokens=torch.zeros((S, R), **i),
+                    traffic=torch.zeros((1, R * (R - 1)), dtype=torch.float64, device=dev))
+
+    def step(m, scratch):
+        sums = dict(d_counts=m["counts"], d_routed=m["routed"])
+        B.nimble_moe_route(m["x"], m["index"], m["weight"], d_prob_sum=m["prob_sum"],
+                           d_seg_ptr=seg, d_scratch=scratch[0], **sums)
+        B.nimble_moe_balance_loss(m["counts"], m["routed"], m["prob_sum"], k, 0.1, m["loss"])
+        B.nimble_moe_route_backward(m["x"], m["index"], m["weight"], m["grad"], d_grad_weight=m["gw"],
+                                    alpha=0.1, d_grad_loss=gl, d_seg_ptr=seg, **sums)
+        B.nimble_moe_counts(m["index"], E, m["counts2"], d_expert_rank=place, d_rank_tokens=m["tokens"],
+                            d_seg_ptr=seg, d_scratch=scratch[1])
+        B.nimble_moe_traffic(1, m["tokens"], 512, m["traffic"])
+
+    def scratch():
+        return [torch.empty(n, dtype=torch.uint8, device=dev)
+                for n in (B.nimble_moe_route_scratch_bytes(T, E, S), B.nimble_moe_counts_scratch_bytes(T, k, E, R, S))]
+
+    eager, mine = memory(), scratch()
+    step(eager, mine)
+    torch.cuda.synchronize()
+    graphs = []
+    for own in (True, False):                              # with scratch given, and from the graph's pool
+        m, sc = memory(), scratch() if own else [None, None]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(m, sc)
+        graphs.append((g, m, sc))
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(1)
+    for turn in range(4):
+        for g, m, _ in graphs:
+            m["x"].copy_(torch.randn((T, E), generator=gen, device=dev))
+            m["gw"].copy_(torch.randn((T, k), generator=gen, device=dev))
+        for g, _, _ in graphs:
+            g.replay()
+        for _, m, _ in graphs:
+            eager["x"].copy_(m["x"])
+            eager["gw"].copy_(m["gw"])
+            step(eager, mine)
+            torch.cuda.synchronize()
+            for n in m:
+                assert torch.equal(m[n], eager[n]), (turn, n)
+
+
+def test_calls_on_two_streams(B):
+    import torch
+    rng = np.random.default_rng(6)
+    xs = [logits(rng, 900, 256, "float32") for _ in range(2)]
+    refs = [run(B, x, 8, sigmoid=True) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    outs = []
+    for x, s in zip(xs, streams):
+        o = dict(index=torch.zeros((900, 8), dtype=torch.int32, device="cuda:0"),
+                 weight=torch.zeros((900, 8), device="cuda:0"),
+                 counts=torch.zeros((1, 256), dtype=torch.int32, device="cuda:0"),
+                 routed=torch.zeros(1, dtype=torch.int32, device="cuda:0"),
+                 prob_sum=torch.zeros((1, 256), device="cuda:0"))
+        outs.append(o)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, s, o in zip(xs, streams, outs):
+            B.nimble_moe_route(x, o["index"], o["weight"], sigmoid=True, d_counts=o["counts"],
+                               d_routed=o["routed"], d_prob_sum=o["prob_sum"], stream=s)
+    torch.cuda.synchronize()
+    for o, r in zip(outs, refs):
+        for n in o:
+            assert np.array_equal(o[n].cpu().numpy(), r[n]), n
+
+
+def test_binding_refuses_what_does_not_fit(B):
+    import torch
+    x = torch.zeros((4, 8), device="cuda:0")
+    i = torch.zeros((4, 2), dtype=torch.int32, device="cuda:0")
+    w = torch.zeros((4, 2), device="cuda:0")
+    for bad in (dict(d_bias=torch.zeros(7, device="cuda:0")), dict(d_keep=torch.zeros(4, device="cuda:0")),
+                dict(d_bias=torch.zeros(8, dtype=torch.float64, device="cuda:0")),
+                dict(d_bias=torch.zeros(8)), dict(d_bias=torch.zeros(16, device="cuda:0")[::2])):
+        with pytest.raises(ValueError):
+            B.nimble_moe_route(x, i, w, **bad)
+    with pytest.raises(ValueError):
+        B.nimble_moe_route(x.t(), torch.zeros((8, 2), dtype=torch.int32, device="cuda:0"),
+                           torch.zeros((8, 2), device="cuda:0"))
+    with pytest.raises(ValueError):
+        B.nimble_moe_route(x[:1].expand(4, 8), i, w)
+    with pytest.raises(ValueError):
+        B.nimble_moe_route(x, i.long(), w)
+    c, r, p = (torch.zeros((1, 8), dtype=torch.int32, device="cuda:0"),
+               torch.zeros(1, dtype=torch.int32, device="cuda:0"), torch.zeros((1, 8), device="cuda:0"))
+    with pytest.raises(B.NimbleError) as e:
+        B.nimble_moe_route(x, i, w, d_counts=c, d_routed=r, d_prob_sum=p,
+                           d_scratch=torch.zeros(16, dtype=torch.uint8, device="cuda:0"))
+    assert e.value.status == B.NIMBLE_ERR_INVALID
+    with pytest.raises(B.NimbleError):
+        B.nimble_moe_route(x, i, w, d_counts=c)
+    with pytest.raises(B.NimbleError):
+        B.nimble_moe_route(torch.zeros((4, 4096), device="cuda:0"), i, w)
+    with pytest.raises(ValueError):
+        B.nimble_moe_traffic(2, torch.zeros((1, 4, 4), dtype=torch.int32, device="cuda:0"), 2.0,
+                             torch.zeros((2, 12), dtype=torch.float64, device="cuda:0"))
