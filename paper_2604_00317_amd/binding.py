@@ -379,77 +379,108 @@ def nimble_plan_quantize(topo: Topo, d_traffic, d_splits, iters: int, chi: int,
 
 # ---- routing (include/nimble_moe.h) -----------------------------------------------------------
 
-class _Call:
-    """The GPU and the stream of a call: every tensor is on the GPU of the first one, which is made
-    current for the call.  A stream of None is the current one of that GPU."""
+# These calls are a few microseconds of GPU work each, so their checks are short: a tensor is looked
+# at once per call, and torch is asked for the bare stream.
 
-    def __init__(self, first, stream):
-        import torch
-        if not isinstance(first, torch.Tensor) or not first.is_cuda:
-            raise TypeError("routing operators take device tensors")
-        self.device = first.device
-        self.given = stream
+def _moe_wrong(t, dtype, numel, gpu, what):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a device tensor")
+    if t.get_device() != gpu:
+        raise ValueError(f"{what} must be on cuda:{gpu}, like the first tensor of the call")
+    raise ValueError(f"{what} must be contiguous {dtype} with {numel} elements")
+
+
+def _moe_ptr(t, dtype, numel, gpu, what):
+    """Pointer of a contiguous tensor on that GPU; None stays None."""
+    if t is None:
+        return None
+    try:
+        if (t.dtype is dtype and t.numel() == numel and t.get_device() == gpu
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _moe_wrong(t, dtype, numel, gpu, what)
+
+
+def _moe_rows(t, dtype, rows, cols, gpu, what):
+    """Pointer and row stride of a matrix whose rows are contiguous and do not overlap."""
+    if t.dtype is not dtype or t.get_device() != gpu or t.shape != (rows, cols):
+        _moe_wrong(t, dtype, rows * cols, gpu, what)
+    if rows < 2 or t.is_contiguous():
+        if rows == 1 and cols > 1 and t.stride(1) != 1:
+            raise ValueError(f"rows of {what} must be contiguous")
+        return t.data_ptr(), cols
+    if (cols > 1 and t.stride(1) != 1) or t.stride(0) < cols:
+        raise ValueError(f"rows of {what} must be contiguous and must not overlap")
+    return t.data_ptr(), t.stride(0)
+
+
+def _moe_gpu(t, what):
+    """Index of the GPU the first tensor of a call is on; all others have to be there."""
+    try:
+        gpu = t.get_device()
+    except AttributeError:
+        gpu = -1
+    if gpu < 0:
+        raise TypeError(f"{what} must be a device tensor")
+    return gpu
+
+
+def _moe_stream(stream, gpu):
+    import torch
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(gpu)
+    if stream.device.index != gpu:
+        raise ValueError("the stream is on another GPU than the tensors")
+    return stream.cuda_stream
+
+
+def _moe_scratch(t, nbytes, gpu, stream):
+    """(pointer, bytes, owner) of scratch memory: the tensor given, or memory of the call's own
+    stream, which torch hands out again only behind the call's work."""
+    import torch
+    if nbytes < 0:
+        return None, 0, None                 # sizes the library refuses: it says why
+    if t is None:
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        elif stream.device != self.device:
-            raise ValueError("the stream is on another device than the tensors")
-        self.stream = stream.cuda_stream
-
-    def ptr(self, t, dtype, shape, what):
-        """Pointer of a contiguous tensor of that shape; None stays None."""
-        if t is None:
-            return None
-        if t.device != self.device:
-            raise ValueError(f"{what} must be on {self.device}")
-        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous {dtype} of shape {shape}")
-        return t.data_ptr()
-
-    def matrix(self, t, dtype, shape, what):
-        """Pointer and row stride of a matrix whose rows are contiguous."""
-        if t.device != self.device:
-            raise ValueError(f"{what} must be on {self.device}")
-        if t.dtype != dtype or tuple(t.shape) != shape or \
-                (shape[0] > 0 and shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{what} must be {dtype} of shape {shape} with contiguous rows")
-        stride = t.stride(0) if shape[0] > 1 else shape[1]
-        if stride < shape[1]:
-            raise ValueError(f"rows of {what} must not overlap")
-        return t.data_ptr(), stride
-
-    def scratch(self, t, nbytes):
-        """(pointer, bytes, owner) of scratch memory: the tensor given, or memory of the call's own
-        stream, which torch hands out again only behind the call's work."""
-        import torch
-        if nbytes < 0:
-            return None, 0, None             # sizes the library refuses: it says why
-        if t is None:
-            if self.given is None:
-                t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            else:
-                with torch.cuda.stream(self.given):
-                    t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        elif t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"d_scratch must be contiguous and on {self.device}")
-        return t.data_ptr(), t.numel() * t.element_size(), t
-
-    def run(self, fn, *args):
-        import torch
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(*args, self.stream))
+            t = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", gpu))
         else:
-            with torch.cuda.device(self.device):
-                _check(fn(*args, self.stream))
+            with torch.cuda.stream(stream):
+                t = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", gpu))
+        return t.data_ptr(), nbytes, t
+    if t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"d_scratch must be contiguous and on cuda:{gpu}")
+    return t.data_ptr(), t.numel() * t.element_size(), t
+
+
+def _moe_run(gpu, fn, *args):
+    import torch
+    if torch._C._cuda_getDevice() == gpu:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(gpu):
+            status = fn(*args)
+    if status != NIMBLE_OK:
+        raise NimbleError(status, nimble_last_error())
 
 
 def _moe_dtype(t):
     import torch
-    kinds = {torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16, torch.bfloat16: NIMBLE_BF16}
-    if t.dtype not in kinds:
+    kind = {torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16,
+            torch.bfloat16: NIMBLE_BF16}.get(t.dtype)
+    if kind is None:
         raise ValueError("d_logits must be float32, float16 or bfloat16")
     if t.dim() != 2:
         raise ValueError("d_logits must be [tokens][experts]")
-    return kinds[t.dtype]
+    return kind
+
+
+def _moe_top_k(d_index, tokens):
+    if d_index.dim() != 2 or d_index.size(0) != tokens:
+        raise ValueError("d_index must be [tokens][top_k]")
+    return d_index.size(1)
 
 
 def _moe_flags(sigmoid: bool, renorm: bool) -> int:
@@ -461,33 +492,34 @@ def _moe_segments(d_seg_ptr) -> int:
 
 
 def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, renorm: bool = True,
-                     scale: float = 1.0, d_bias=None, d_keep=None, d_seg_ptr=None,
-                     d_counts=None, d_routed=None, d_prob_sum=None, d_scratch=None,
-                     stream=None) -> None:
+                     scale: float = 1.0, d_bias=None, d_keep=None, d_seg_ptr=None, d_counts=None,
+                     d_routed=None, d_prob_sum=None, d_scratch=None, stream=None) -> None:
     """Chooses d_index.shape[1] experts per row of d_logits [tokens][experts] (float32, float16 or
     bfloat16; rows may be strided), with their weights.  d_counts [segments][experts], d_routed
     [segments] and d_prob_sum [segments][experts] are wanted together or not at all."""
     import torch
+    i32, f32 = torch.int32, torch.float32
     lib = load_library()
     kind = _moe_dtype(d_logits)
-    c = _Call(d_logits, stream)
+    gpu = _moe_gpu(d_logits, "d_logits")
     tokens, experts = d_logits.shape
-    top_k = d_index.shape[1] if d_index.dim() == 2 else 0
+    top_k = _moe_top_k(d_index, tokens)
     n_seg = _moe_segments(d_seg_ptr)
-    x, stride = c.matrix(d_logits, d_logits.dtype, (tokens, experts), "d_logits")
+    x, stride = _moe_rows(d_logits, d_logits.dtype, tokens, experts, gpu, "d_logits")
     scratch = nbytes = owner = None
     if d_counts is not None:
-        scratch, nbytes, owner = c.scratch(
-            d_scratch, lib.nimble_moe_route_scratch_bytes(tokens, experts, n_seg))
-    c.run(lib.nimble_moe_route, tokens, experts, top_k, _moe_flags(sigmoid, renorm), kind, x, stride,
-          c.ptr(d_bias, torch.float32, (experts,), "d_bias"),
-          c.ptr(d_keep, torch.uint8, (tokens,), "d_keep"), scale, n_seg,
-          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
-          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"),
-          c.ptr(d_weight, torch.float32, (tokens, top_k), "d_weight"),
-          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
-          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
-          c.ptr(d_prob_sum, torch.float32, (n_seg, experts), "d_prob_sum"), scratch, nbytes or 0)
+        scratch, nbytes, owner = _moe_scratch(
+            d_scratch, lib.nimble_moe_route_scratch_bytes(tokens, experts, n_seg), gpu, stream)
+    _moe_run(gpu, lib.nimble_moe_route, tokens, experts, top_k, _moe_flags(sigmoid, renorm), kind, x,
+             stride, _moe_ptr(d_bias, f32, experts, gpu, "d_bias"),
+             _moe_ptr(d_keep, torch.uint8, tokens, gpu, "d_keep"), scale, n_seg,
+             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
+             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
+             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"),
+             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
+             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
+             _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum"), scratch, nbytes or 0,
+             _moe_stream(stream, gpu))
 
 
 def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 1) -> int:
@@ -498,42 +530,44 @@ def nimble_moe_balance_loss(d_counts, d_routed, d_prob_sum, top_k: int, alpha: f
                             stream=None) -> None:
     """d_loss [segments] from the sums nimble_moe_route gives."""
     import torch
-    c = _Call(d_counts, stream)
+    gpu = _moe_gpu(d_counts, "d_counts")
     if d_counts.dim() != 2:
         raise ValueError("d_counts must be [segments][experts]")
     n_seg, experts = d_counts.shape
-    c.run(load_library().nimble_moe_balance_loss, n_seg, experts, top_k,
-          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
-          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
-          c.ptr(d_prob_sum, torch.float32, (n_seg, experts), "d_prob_sum"), alpha,
-          c.ptr(d_loss, torch.float32, (n_seg,), "d_loss"))
+    _moe_run(gpu, load_library().nimble_moe_balance_loss, n_seg, experts, top_k,
+             _moe_ptr(d_counts, torch.int32, n_seg * experts, gpu, "d_counts"),
+             _moe_ptr(d_routed, torch.int32, n_seg, gpu, "d_routed"),
+             _moe_ptr(d_prob_sum, torch.float32, n_seg * experts, gpu, "d_prob_sum"), alpha,
+             _moe_ptr(d_loss, torch.float32, n_seg, gpu, "d_loss"), _moe_stream(stream, gpu))
 
 
-def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *,
-                              sigmoid: bool = False, renorm: bool = True, scale: float = 1.0,
-                              d_keep=None, d_seg_ptr=None, d_grad_weight=None, alpha: float = 0.0,
-                              d_counts=None, d_routed=None, d_grad_loss=None,
-                              stream=None) -> None:
+def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sigmoid: bool = False,
+                              renorm: bool = True, scale: float = 1.0, d_keep=None, d_seg_ptr=None,
+                              d_grad_weight=None, alpha: float = 0.0, d_counts=None, d_routed=None,
+                              d_grad_loss=None, stream=None) -> None:
     """Gradient of the logits from those of weights and loss, with the flags, scale, d_keep and
     segments of the call of nimble_moe_route that gave d_index and d_weight."""
     import torch
+    i32, f32 = torch.int32, torch.float32
     kind = _moe_dtype(d_logits)
-    c = _Call(d_logits, stream)
+    gpu = _moe_gpu(d_logits, "d_logits")
     tokens, experts = d_logits.shape
-    top_k = d_index.shape[1] if d_index.dim() == 2 else 0
+    top_k = _moe_top_k(d_index, tokens)
     n_seg = _moe_segments(d_seg_ptr)
-    x, stride = c.matrix(d_logits, d_logits.dtype, (tokens, experts), "d_logits")
-    dx, grad_stride = c.matrix(d_grad_logits, d_logits.dtype, (tokens, experts), "d_grad_logits")
-    c.run(load_library().nimble_moe_route_backward, tokens, experts, top_k,
-          _moe_flags(sigmoid, renorm), kind, x, stride,
-          c.ptr(d_keep, torch.uint8, (tokens,), "d_keep"), scale, n_seg,
-          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
-          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"),
-          c.ptr(d_weight, torch.float32, (tokens, top_k), "d_weight"),
-          c.ptr(d_grad_weight, torch.float32, (tokens, top_k), "d_grad_weight"), alpha,
-          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
-          c.ptr(d_routed, torch.int32, (n_seg,), "d_routed"),
-          c.ptr(d_grad_loss, torch.float32, (n_seg,), "d_grad_loss"), dx, grad_stride)
+    x, stride = _moe_rows(d_logits, d_logits.dtype, tokens, experts, gpu, "d_logits")
+    dx, grad_stride = _moe_rows(d_grad_logits, d_logits.dtype, tokens, experts, gpu,
+                                "d_grad_logits")
+    _moe_run(gpu, load_library().nimble_moe_route_backward, tokens, experts, top_k,
+             _moe_flags(sigmoid, renorm), kind, x, stride,
+             _moe_ptr(d_keep, torch.uint8, tokens, gpu, "d_keep"), scale, n_seg,
+             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
+             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
+             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"),
+             _moe_ptr(d_grad_weight, f32, tokens * top_k, gpu, "d_grad_weight"), alpha,
+             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
+             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
+             _moe_ptr(d_grad_loss, f32, n_seg, gpu, "d_grad_loss"), dx, grad_stride,
+             _moe_stream(stream, gpu))
 
 
 def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=None,
@@ -541,21 +575,23 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
     """Slots per expert (d_counts [segments][experts]) and distinct tokens per destination GPU
     (d_rank_tokens [segments][ranks], by d_expert_rank [experts]) of routed tokens."""
     import torch
+    i32 = torch.int32
     lib = load_library()
-    c = _Call(d_index, stream)
-    if d_index.dim() != 2:
-        raise ValueError("d_index must be [tokens][top_k]")
-    tokens, top_k = d_index.shape
+    gpu = _moe_gpu(d_index, "d_index")
+    tokens = d_index.size(0)
+    top_k = _moe_top_k(d_index, tokens)
     n_seg = _moe_segments(d_seg_ptr)
-    ranks = 0 if d_rank_tokens is None else d_rank_tokens.shape[-1]
-    scratch, nbytes, owner = c.scratch(
-        d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg))
-    c.run(lib.nimble_moe_counts, tokens, top_k,
-          c.ptr(d_index, torch.int32, (tokens, top_k), "d_index"), experts, n_seg,
-          c.ptr(d_seg_ptr, torch.int32, (n_seg + 1,), "d_seg_ptr"),
-          c.ptr(d_expert_rank, torch.int32, (experts,), "d_expert_rank"), ranks,
-          c.ptr(d_counts, torch.int32, (n_seg, experts), "d_counts"),
-          c.ptr(d_rank_tokens, torch.int32, (n_seg, ranks), "d_rank_tokens"), scratch, nbytes)
+    ranks = 0 if d_rank_tokens is None else d_rank_tokens.size(-1)
+    scratch, nbytes, owner = _moe_scratch(
+        d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg), gpu,
+        stream)
+    _moe_run(gpu, lib.nimble_moe_counts, tokens, top_k,
+             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"), experts, n_seg,
+             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
+             _moe_ptr(d_expert_rank, i32, experts, gpu, "d_expert_rank"), ranks,
+             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
+             _moe_ptr(d_rank_tokens, i32, n_seg * ranks, gpu, "d_rank_tokens"), scratch, nbytes,
+             _moe_stream(stream, gpu))
 
 
 def nimble_moe_counts_scratch_bytes(tokens: int, top_k: int, experts: int, n_ranks: int = 0,
@@ -569,18 +605,18 @@ def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traf
     """Demand vectors d_traffic [batch][n_comm] of d_rank_tokens, [batch][ranks][ranks] or the
     [batch * ranks][ranks] that nimble_moe_counts fills with a segment per source GPU."""
     import torch
-    c = _Call(d_rank_tokens, stream)
-    ranks = d_rank_tokens.shape[-1]
-    if d_rank_tokens.numel() != batch * ranks * ranks:
-        raise ValueError("d_rank_tokens must be [batch][ranks][ranks]")
+    i32 = torch.int32
+    gpu = _moe_gpu(d_rank_tokens, "d_rank_tokens")
+    ranks = d_rank_tokens.size(-1)
     if batch < 1 or d_traffic.numel() % batch:
         raise ValueError("d_traffic must be [batch][commodities]")
     n_comm = d_traffic.numel() // batch
-    c.run(load_library().nimble_moe_traffic, batch, ranks,
-          c.ptr(d_rank_tokens, torch.int32, tuple(d_rank_tokens.shape), "d_rank_tokens"),
-          bytes_per_token, n_comm, c.ptr(d_src, torch.int32, (n_comm,), "d_src"),
-          c.ptr(d_dst, torch.int32, (n_comm,), "d_dst"), NIMBLE_MOE_WAY_BACK if way_back else 0,
-          c.ptr(d_traffic, torch.float64, tuple(d_traffic.shape), "d_traffic"))
+    _moe_run(gpu, load_library().nimble_moe_traffic, batch, ranks,
+             _moe_ptr(d_rank_tokens, i32, batch * ranks * ranks, gpu, "d_rank_tokens"),
+             bytes_per_token, n_comm, _moe_ptr(d_src, i32, n_comm, gpu, "d_src"),
+             _moe_ptr(d_dst, i32, n_comm, gpu, "d_dst"), NIMBLE_MOE_WAY_BACK if way_back else 0,
+             _moe_ptr(d_traffic, torch.float64, batch * n_comm, gpu, "d_traffic"),
+             _moe_stream(stream, gpu))
 
 
 def nimble_debug_run_phase(topo: Topo, phase: int, reps: int, d_traffic, stream=None) -> None:
