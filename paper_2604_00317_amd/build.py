@@ -11,7 +11,7 @@ SOURCES = ["api.hip", "kernels_stream.hip", "kernels_resident.hip",
            "kernels_persistent.hip", "kernels_alg1.hip", "kernels_post.hip", "kernels_adaptive.hip", "kernels_probe.hip",
            "kernels_patch_single.hip", "kernels_patch_sum.hip", "kernels_patch_max.hip",
            "kernels_patch_adaptive.hip", "kernels_blocks_sum.hip", "kernels_blocks_max.hip",
-           "kernels_moe.hip", "api_moe.hip", "host_topo.cpp", "host_patch.cpp"]
+           "kernels_moe_f32.hip", "kernels_moe_f16.hip", "kernels_moe_bf16.hip", "kernels_moe.hip", "api_moe.hip", "host_topo.cpp", "host_patch.cpp"]
 # -ffp-contract=off: one IEEE operation per statement on host and device (no FMA contraction).
 # packed-fp32-ops is switched off for every device compile of this build.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

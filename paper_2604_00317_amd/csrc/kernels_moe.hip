@@ -1,432 +1,23 @@
-// Routing kernels: choice of experts with its sums, balance loss, gradient of the logits, counts
-// per expert and destination GPU, demand vectors (definitions in include/nimble_moe.h).
+// Routing kernels that work on sums and indices: end of the sums, balance loss, counts per expert and
+// destination GPU, demand vectors (definitions in include/nimble_moe.h), and the launchers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
-#include "../../include/nimble_moe.h"
 #include "kernels_moe.hpp"
-#include "wave_ops.hpp"
+#include "moe_device.hpp"
 
 namespace nimble::moe {
 
+// one per element type, kernels_moe_*.hip
+hipError_t route_f32(const RouteArgs &a, hipStream_t stream);
+hipError_t route_f16(const RouteArgs &a, hipStream_t stream);
+hipError_t route_bf16(const RouteArgs &a, hipStream_t stream);
+hipError_t backward_f32(const BackwardArgs &a, hipStream_t stream);
+hipError_t backward_f16(const BackwardArgs &a, hipStream_t stream);
+hipError_t backward_bf16(const BackwardArgs &a, hipStream_t stream);
+
 namespace {
-
-constexpr float kInf = __builtin_inff();
-constexpr int kStatWaves = 8;        // waves of a workgroup that makes sums
-constexpr int kRowWaves = 4;         // of one that does not
-
-// ---- element types ---------------------------------------------------------------------------
-
-struct F32 {
-    using Raw = float;
-    static __device__ __forceinline__ float up(float v) { return v; }
-    static __device__ __forceinline__ float down(float v) { return v; }
-};
-struct F16 {
-    using Raw = uint16_t;
-    static __device__ __forceinline__ float up(uint16_t v)
-    {
-        return static_cast<float>(__builtin_bit_cast(_Float16, v));
-    }
-    static __device__ __forceinline__ uint16_t down(float v)
-    {
-        return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
-    }
-};
-struct BF16 {
-    using Raw = uint16_t;
-    static __device__ __forceinline__ float up(uint16_t v)
-    {
-        return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
-    }
-    static __device__ __forceinline__ uint16_t down(float v)
-    {
-        return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-    }
-};
-
-// A row lies in a wave as V values per lane, in groups of W neighbours (one load each): lane l
-// has columns q * 64 W + l W + 0 .. W-1 for q = 0 .. V/W - 1.
-template <int V>
-constexpr int group_width() { return V < 4 ? V : 4; }
-
-template <class D, int W>
-struct alignas(sizeof(typename D::Raw) * W) Group {
-    typename D::Raw v[W];
-};
-
-// Columns beyond the row's end come as -inf, like masked ones.  `whole`: groups inside the row are
-// aligned to their size.
-template <class D, int V>
-__device__ __forceinline__ void load_row(const typename D::Raw *row, int experts, int lane,
-                                         bool whole, float (&x)[V])
-{
-    constexpr int W = group_width<V>();
-#pragma unroll
-    for (int q = 0; q < V / W; ++q) {
-        const int col = q * (kWave * W) + lane * W;
-        if (whole && col + W <= experts) {
-            const auto g = *reinterpret_cast<const Group<D, W> *>(row + col);
-#pragma unroll
-            for (int i = 0; i < W; ++i) x[q * W + i] = D::up(g.v[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) x[q * W + i] = col + i < experts ? D::up(row[col + i]) : -kInf;
-        }
-    }
-}
-
-template <class D, int V>
-__device__ __forceinline__ void store_row(typename D::Raw *row, int experts, int lane, bool whole,
-                                          const float (&x)[V])
-{
-    constexpr int W = group_width<V>();
-#pragma unroll
-    for (int q = 0; q < V / W; ++q) {
-        const int col = q * (kWave * W) + lane * W;
-        if (whole && col + W <= experts) {
-            Group<D, W> g;
-#pragma unroll
-            for (int i = 0; i < W; ++i) g.v[i] = D::down(x[q * W + i]);
-            *reinterpret_cast<Group<D, W> *>(row + col) = g;
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i)
-                if (col + i < experts) row[col + i] = D::down(x[q * W + i]);
-        }
-    }
-}
-
-// ---- reductions over lanes -------------------------------------------------------------------
-
-struct TwoF32 {
-    float a, b;
-};
-__device__ __forceinline__ TwoF32 rows_f32(float v)          // both rows of a pair of rows
-{
-    const int i = __builtin_bit_cast(int, v);
-    const auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
-    return {__builtin_bit_cast(float, static_cast<int>(r[0])),
-            __builtin_bit_cast(float, static_cast<int>(r[1]))};
-}
-__device__ __forceinline__ TwoF32 halves_f32(float v)        // both halves of the wave
-{
-    const int i = __builtin_bit_cast(int, v);
-    const auto r = __builtin_amdgcn_permlane32_swap(i, i, false, false);
-    return {__builtin_bit_cast(float, static_cast<int>(r[0])),
-            __builtin_bit_cast(float, static_cast<int>(r[1]))};
-}
-template <int CTRL>
-__device__ __forceinline__ float dpp_f32(float v)
-{
-    return __builtin_bit_cast(float, dpp_i32<CTRL>(__builtin_bit_cast(int, v)));
-}
-
-// over aligned groups of 16 lanes, and over the wave; the same bits in all lanes
-__device__ __forceinline__ float max16(float v)
-{
-    v = fmaxf(v, dpp_f32<kDppXor1>(v));
-    v = fmaxf(v, dpp_f32<kDppXor2>(v));
-    v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
-    return fmaxf(v, dpp_f32<kDppMirror>(v));
-}
-__device__ __forceinline__ float sum16(float v)
-{
-    v = v + dpp_f32<kDppXor1>(v);
-    v = v + dpp_f32<kDppXor2>(v);
-    v = v + dpp_f32<kDppHalfMirror>(v);
-    return v + dpp_f32<kDppMirror>(v);
-}
-__device__ __forceinline__ float max64(float v)
-{
-    v = max16(v);
-    const TwoF32 r = rows_f32(v);
-    const TwoF32 h = halves_f32(fmaxf(r.a, r.b));
-    return fmaxf(h.a, h.b);
-}
-__device__ __forceinline__ float sum64(float v)
-{
-    v = sum16(v);
-    const TwoF32 r = rows_f32(v);
-    const TwoF32 h = halves_f32(r.a + r.b);
-    return h.a + h.b;
-}
-
-__device__ __forceinline__ float uniform(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
-}
-__device__ __forceinline__ float of_lane(float v, int lane)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
-}
-
-// exp by the hardware's exp2: off by 2^-23 |x| and a step or so, relative; results below 2^-126 are 0
-__device__ __forceinline__ float exp_of(float x)
-{
-    return __builtin_amdgcn_exp2f(x * 1.44269504f);
-}
-
-// Sigmoids are summed and compared as s(x) exp(-shift) = exp(min(x, 0) - shift) / (1 + exp(-|x|)), shift
-// = 0 unless the row's largest logit is so low that all sigmoids would vanish in 32 bits.
-__device__ __forceinline__ float sigmoid_shift(float top) { return top < -60.0f ? top : 0.0f; }
-__device__ __forceinline__ float shifted_sigmoid(float x, float shift)
-{
-    const float e = exp_of(-fabsf(x));
-    float n = x > 0.0f ? 1.0f : e;
-    if (shift != 0.0f) n = exp_of(x - shift);
-    return n * __builtin_amdgcn_rcpf(1.0f + e);
-}
-
-// ---- segments --------------------------------------------------------------------------------
-
-__device__ __forceinline__ int offset(const Rows &r, int s)
-{
-    return min(max(r.seg_ptr[s], 0), r.tokens);
-}
-__device__ __forceinline__ int begin_of(const Rows &r, int s) { return r.seg_ptr ? offset(r, s) : 0; }
-__device__ __forceinline__ int end_of(const Rows &r, int s)
-{
-    return r.seg_ptr ? offset(r, s + 1) : r.tokens;
-}
-
-// The first segment that ends behind `row`, by a search with 64 tries at a time (a round trip to
-// memory each).  All lanes of the wave are active and get the same answer.
-__device__ __forceinline__ int first_segment(const Rows &r, int row, int lane)
-{
-    if (!r.seg_ptr) return 0;
-    int at = 0, n = r.segments;
-    while (n > 0) {
-        const int step = (n + kWave - 1) / kWave;
-        const int s = at + lane * step + step - 1;
-        const bool behind = s >= at + n || r.seg_ptr[s + 1] > row;
-        const unsigned long long hit = __ballot(behind);
-        if (hit == 0) return at + n;
-        const int to = at + (__ffsll(hit) - 1) * step;
-        n = min(step - 1, at + n - to);
-        at = to;
-    }
-    return at;
-}
-
-// ---- choice ----------------------------------------------------------------------------------
-
-// The top_k largest keys of a row, lane j gets column and logit of slot j (-1 and -inf where there
-// is none).  Per slot: the largest key of the wave (each lane has the largest of every group of W
-// at hand), the first group and lane that hold it in column order, and that one key taken out.
-// All of the bookkeeping is in scalars: the lanes' answers are ballots.
-template <int V>
-__device__ __forceinline__ void choose(float (&key)[V], const float (&x)[V], int top_k, int lane,
-                                       int &index, float &logit)
-{
-    constexpr int W = group_width<V>(), Q = V / W;
-    float top[Q];
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        top[q] = key[q * W];
-#pragma unroll
-        for (int i = 1; i < W; ++i) top[q] = fmaxf(top[q], key[q * W + i]);
-    }
-    index = -1;
-    logit = -kInf;
-    for (int slot = 0; slot < top_k; ++slot) {
-        float best = top[0];
-#pragma unroll
-        for (int q = 1; q < Q; ++q) best = fmaxf(best, top[q]);
-        best = uniform(max64(best));
-        if (best == -kInf) return;
-        bool found = false;
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const unsigned long long any = __ballot(top[q] == best);
-            if (found || any == 0) continue;
-            found = true;
-            const int owner = __ffsll(any) - 1;
-            const unsigned long long bit = 1ull << owner;
-            bool taken = false;
-            float value = -kInf;
-            int col = q * (kWave * W) + owner * W;
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const bool here = !taken && (__ballot(key[q * W + i] == best) & bit) != 0;
-                if (here) {
-                    value = of_lane(x[q * W + i], owner);
-                    col += i;
-                    key[q * W + i] = lane == owner ? -kInf : key[q * W + i];
-                }
-                taken = taken || here;
-            }
-            top[q] = key[q * W];
-#pragma unroll
-            for (int i = 1; i < W; ++i) top[q] = fmaxf(top[q], key[q * W + i]);
-            if (lane == slot) {
-                index = col;
-                logit = value;
-            }
-        }
-    }
-}
-
-// One row: choice, weights, statistics; p gets the probabilities (0 or NaN where there are none).
-// Returns whether the row has a choice.
-template <class D, int V>
-__device__ __forceinline__ bool route_row(const RouteArgs &a, int64_t row, int lane, bool whole,
-                                          const float (&bias)[V], float (&p)[V], int &index)
-{
-    const bool sigmoid = (a.flags & NIMBLE_MOE_SIGMOID) != 0;
-    const bool renorm = (a.flags & NIMBLE_MOE_RENORM) != 0;
-    const int64_t slot = row * a.top_k + lane;
-    if (a.keep && a.keep[row] == 0) {
-        index = -1;
-#pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = 0.0f;
-        if (lane < a.top_k) {
-            a.index[slot] = -1;
-            a.weight[slot] = 0.0f;
-        }
-        return false;
-    }
-    float x[V], key[V];
-    load_row<D, V>(static_cast<const typename D::Raw *>(a.logits) + row * a.stride, a.experts, lane,
-                   whole, x);
-    float top = x[0];
-#pragma unroll
-    for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-    top = max64(top);
-    const float shift = sigmoid ? sigmoid_shift(top == -kInf ? 0.0f : top) : (top == -kInf ? 0.0f : top);
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        p[j] = sigmoid ? shifted_sigmoid(x[j], shift) : exp_of(x[j] - shift);
-        sum = sum + p[j];
-    }
-    sum = sum64(sum);
-    const bool bad = !(sum == sum) || top == kInf;
-    const bool empty = !bad && top == -kInf;
-    const float inv = bad ? __builtin_nanf("") : (empty ? 0.0f : 1.0f / sum);
-#pragma unroll
-    for (int j = 0; j < V; ++j) p[j] = p[j] * inv;
-
-    index = -1;
-    float logit = -kInf;
-    if (!bad && !empty) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float k = x[j] + bias[j];
-            key[j] = x[j] == -kInf || !(k == k) ? -kInf : k;
-        }
-        choose<V>(key, x, a.top_k, lane, index, logit);
-    }
-    float w;
-    if (renorm) {
-        const float t = max16(logit);
-        const float u = sigmoid ? shifted_sigmoid(logit, sigmoid_shift(t)) : exp_of(logit - t);
-        w = u / sum16(u);
-    } else {
-        w = sigmoid ? shifted_sigmoid(logit, 0.0f) : exp_of(logit - shift) * inv;
-    }
-    w = bad ? __builtin_nanf("") : (index < 0 ? 0.0f : w * a.scale);
-    if (lane < a.top_k) {
-        a.index[slot] = index;
-        a.weight[slot] = w;
-    }
-    const bool chosen = __builtin_amdgcn_readfirstlane(index) >= 0;
-    if (!bad && !chosen) {                       // nothing but keys of -inf
-#pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = 0.0f;
-    }
-    return chosen;
-}
-
-template <int V>
-__device__ __forceinline__ void load_bias(const RouteArgs &a, int lane, float (&bias)[V])
-{
-    constexpr int W = group_width<V>();
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int col = (j / W) * (kWave * W) + lane * W + j % W;
-        bias[j] = a.bias && col < a.experts ? a.bias[col] : 0.0f;   // (+0: the keys' zeros are +0)
-    }
-}
-
-// A wave per row, no sums.
-template <class D, int V>
-__global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, bool whole)
-{
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    float bias[V];
-    load_bias<V>(a, lane, bias);
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRowWaves + wave; row < a.rows.tokens;
-         row += static_cast<int64_t>(gridDim.x) * kRowWaves) {
-        if (a.rows.seg_ptr) {
-            const int s = first_segment(a.rows, static_cast<int>(row), lane);
-            if (s >= a.rows.segments || begin_of(a.rows, s) > row) continue;
-        }
-        float p[V];
-        int index;
-        route_row<D, V>(a, row, lane, whole, bias, p, index);
-    }
-}
-
-// A workgroup per chunk, a wave per row in turn; probabilities are summed in registers, slots
-// counted in LDS, and the waves' sums added in order at the end of every part.
-template <class D, int V>
-__global__ __launch_bounds__(kStatWaves *kWave) void k_route_sums(RouteArgs a, bool whole)
-{
-    constexpr int C = V * kWave;
-    __shared__ float sums[kStatWaves][C];
-    __shared__ int hits[C];
-    __shared__ int routed[kStatWaves];
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
-    const int lo = static_cast<int>(first);
-    const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
-    float bias[V];
-    load_bias<V>(a, lane, bias);
-    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
-        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
-        if (begin_of(a.rows, s) >= hi) break;
-        if (from >= to) continue;
-        for (int c = threadIdx.x; c < C; c += kStatWaves * kWave) hits[c] = 0;
-        __syncthreads();
-        float acc[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.0f;
-        int n = 0;
-        for (int row = from + wave; row < to; row += kStatWaves) {
-            float p[V];
-            int index;
-            n += route_row<D, V>(a, row, lane, whole, bias, p, index) ? 1 : 0;
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] = acc[j] + p[j];
-            if (lane < a.top_k && index >= 0) atomicAdd(&hits[index], 1);
-        }
-        constexpr int W = group_width<V>();
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            sums[wave][(j / W) * (kWave * W) + lane * W + j % W] = acc[j];
-        if (lane == 0) routed[wave] = n;
-        __syncthreads();
-        const int64_t part = static_cast<int64_t>(blockIdx.x) + s;
-        for (int c = threadIdx.x; c < a.experts; c += kStatWaves * kWave) {
-            float t = sums[0][c];
-#pragma unroll
-            for (int w = 1; w < kStatWaves; ++w) t = t + sums[w][c];
-            a.part_prob[part * a.experts + c] = t;
-            a.part_count[part * a.experts + c] = hits[c];
-        }
-        if (threadIdx.x == 0) {
-            int t = 0;
-            for (int w = 0; w < kStatWaves; ++w) t += routed[w];
-            a.part_routed[part] = t;
-        }
-        __syncthreads();
-    }
-}
 
 constexpr int kFinishWaves = 16;
 
@@ -493,107 +84,6 @@ __global__ __launch_bounds__(256) void k_balance_loss(int experts, double unit, 
         const double n = static_cast<double>(routed[blockIdx.x]);
         t = ((part[0] + part[1]) + part[2]) + part[3];
         loss[blockIdx.x] = routed[blockIdx.x] == 0 ? 0.0f : static_cast<float>(unit * t / (n * n));
-    }
-}
-
-// ---- gradient --------------------------------------------------------------------------------
-
-template <class D, int V>
-__global__ __launch_bounds__(kStatWaves *kWave) void k_route_backward(BackwardArgs a, bool whole)
-{
-    constexpr int W = group_width<V>(), C = V * kWave;
-    __shared__ float slots[kStatWaves][C];       // the weights' part of a wave's row, by column
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
-    const int lo = static_cast<int>(first);
-    const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
-    const bool sigmoid = (a.flags & NIMBLE_MOE_SIGMOID) != 0;
-    const bool renorm = (a.flags & NIMBLE_MOE_RENORM) != 0;
-    float *mine = slots[wave];
-    for (int c = lane; c < C; c += kWave) mine[c] = 0.0f;
-    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
-        if (begin_of(a.rows, s) >= hi) break;
-        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
-        if (from >= to) continue;
-        float coef[V];
-        double unit = 0.0;
-        if (a.counts) {
-            const double n = static_cast<double>(a.routed[s]);
-            if (a.routed[s] != 0)
-                unit = static_cast<double>(a.grad_loss[s]) * static_cast<double>(a.alpha) * a.experts /
-                       (static_cast<double>(a.top_k) * n * n);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int col = (j / W) * (kWave * W) + lane * W + j % W;
-            coef[j] = a.counts && col < a.experts
-                          ? static_cast<float>(unit * a.counts[static_cast<int64_t>(s) * a.experts + col])
-                          : 0.0f;
-        }
-        for (int row = from + wave; row < to; row += kStatWaves) {
-            float x[V];
-            const int64_t at = row;
-            auto *out = static_cast<typename D::Raw *>(a.grad) + at * a.grad_stride;
-            const bool kept = !a.keep || a.keep[row] != 0;
-            const float first_w = kept ? a.weight[at * a.top_k] : 0.0f;
-            int index = -1;
-            float wg = 0.0f, w = 0.0f, g = 0.0f;
-            if (kept && lane < a.top_k) {
-                index = a.index[at * a.top_k + lane];
-                if (static_cast<uint32_t>(index) >= static_cast<uint32_t>(a.experts)) index = -1;
-                if (index >= 0) {
-                    w = a.weight[at * a.top_k + lane];
-                    if (a.grad_weight) g = a.grad_weight[at * a.top_k + lane];
-                    wg = w * g;
-                }
-            }
-            const bool nan = kept && !(first_w == first_w);
-            if (__ballot(index >= 0) == 0) {                     // left out, or without a choice
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[j] = nan ? __builtin_nanf("") : 0.0f;
-                store_row<D, V>(out, a.experts, lane, whole, x);
-                continue;
-            }
-            load_row<D, V>(static_cast<const typename D::Raw *>(a.logits) + at * a.stride, a.experts,
-                           lane, whole, x);
-            const float all = uniform(sum16(wg));
-            const float slope = w * (g - (renorm ? all / a.scale : 0.0f));
-            if (index >= 0) atomicAdd(&mine[index], slope);
-            float top = x[0], sum = 0.0f, rest = 0.0f, p[V], r[V];
-#pragma unroll
-            for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-            top = max64(top);
-            const float shift = sigmoid ? sigmoid_shift(top) : top;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (sigmoid) {
-                    const float e = exp_of(-fabsf(x[j]));
-                    const float d = __builtin_amdgcn_rcpf(1.0f + e);
-                    r[j] = x[j] > 0.0f ? e * d : d;              // 1 - s
-                    p[j] = (shift != 0.0f ? exp_of(x[j] - shift) : (x[j] > 0.0f ? 1.0f : e)) * d;
-                } else {
-                    r[j] = 1.0f;
-                    p[j] = exp_of(x[j] - shift);
-                }
-                sum = sum + p[j];
-                rest = rest + p[j] * coef[j];
-            }
-            const float inv = 1.0f / sum64(sum);
-#pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = p[j] * inv;
-            rest = sum64(rest) * inv;
-            if (!sigmoid && !renorm) rest = rest + all;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int col = (j / W) * (kWave * W) + lane * W + j % W;
-                x[j] = r[j] * (p[j] * (coef[j] - rest) + mine[col]);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (index >= 0) mine[index] = 0.0f;
-            store_row<D, V>(out, a.experts, lane, whole, x);
-        }
     }
 }
 
@@ -700,74 +190,16 @@ __global__ __launch_bounds__(256) void k_traffic(int64_t total, int ranks, const
     traffic[at] = v;
 }
 
-// ---- launches --------------------------------------------------------------------------------
-
-// Rows can be read and written in groups: those inside a row are aligned to their size.
-bool groups_align(const void *base, int64_t stride, int width, int bytes)
-{
-    const auto at = reinterpret_cast<uintptr_t>(base);
-    return at % static_cast<uintptr_t>(width * bytes) == 0 && stride % width == 0;
-}
-
-template <class D, int V>
-hipError_t route_as(const RouteArgs &a, hipStream_t stream)
-{
-    const bool whole = groups_align(a.logits, a.stride, group_width<V>(), sizeof(typename D::Raw));
-    if (!a.counts) {
-        if (a.rows.tokens == 0) return hipSuccess;
-        const int64_t grid = std::min<int64_t>((static_cast<int64_t>(a.rows.tokens) + kRowWaves - 1) / kRowWaves,
-                                               1 << 20);
-        k_route<D, V><<<static_cast<unsigned>(grid), kRowWaves * kWave, 0, stream>>>(a, whole);
-        return hipGetLastError();
-    }
-    if (a.rows.chunks > 0) {
-        k_route_sums<D, V><<<a.rows.chunks, kStatWaves * kWave, 0, stream>>>(a, whole);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    k_route_finish<<<dim3(a.rows.segments, (a.experts + kWave - 1) / kWave), kFinishWaves * kWave, 0,
-                     stream>>>(a);
-    return hipGetLastError();
-}
-
-template <class D, int V>
-hipError_t backward_as(const BackwardArgs &a, hipStream_t stream)
-{
-    constexpr int W = group_width<V>(), B = sizeof(typename D::Raw);
-    if (a.rows.chunks == 0) return hipSuccess;
-    const bool whole = groups_align(a.logits, a.stride, W, B) && groups_align(a.grad, a.grad_stride, W, B);
-    k_route_backward<D, V><<<a.rows.chunks, kStatWaves * kWave, 0, stream>>>(a, whole);
-    return hipGetLastError();
-}
-
-template <class D>
-hipError_t route_of(const RouteArgs &a, hipStream_t stream)
-{
-    if (a.experts <= 64) return route_as<D, 1>(a, stream);
-    if (a.experts <= 128) return route_as<D, 2>(a, stream);
-    if (a.experts <= 256) return route_as<D, 4>(a, stream);
-    if (a.experts <= 512) return route_as<D, 8>(a, stream);
-    if (a.experts <= 1024) return route_as<D, 16>(a, stream);
-    return route_as<D, 32>(a, stream);
-}
-
-template <class D>
-hipError_t backward_of(const BackwardArgs &a, hipStream_t stream)
-{
-    if (a.experts <= 64) return backward_as<D, 1>(a, stream);
-    if (a.experts <= 128) return backward_as<D, 2>(a, stream);
-    if (a.experts <= 256) return backward_as<D, 4>(a, stream);
-    if (a.experts <= 512) return backward_as<D, 8>(a, stream);
-    if (a.experts <= 1024) return backward_as<D, 16>(a, stream);
-    return backward_as<D, 32>(a, stream);
-}
-
 }  // namespace
 
-// About four workgroups per CU, and no fewer rows than waves.
-int32_t route_chunk(int32_t tokens, int32_t)
+// Whole passes of a workgroup's rows, and no more than 1024 chunks with sums to add up: about four
+// workgroups per CU.
+int32_t route_chunk(int32_t tokens, int32_t experts, bool sums)
 {
-    return std::max(kStatWaves, (tokens + 1023) / 1024);
+    const int32_t pass = kRowWaves * (experts <= 256 ? 4 : experts <= 512 ? 2 : 1);
+    const int32_t most = sums ? 1 << 10 : 1 << 20;
+    const int64_t rows = (static_cast<int64_t>(tokens) + most - 1) / most;
+    return static_cast<int32_t>((std::max<int64_t>(rows, 1) + pass - 1) / pass * pass);
 }
 
 int32_t count_chunk(int32_t tokens, int32_t)
@@ -777,9 +209,16 @@ int32_t count_chunk(int32_t tokens, int32_t)
 
 hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream)
 {
-    if (dtype == NIMBLE_F32) return route_of<F32>(a, stream);
-    if (dtype == NIMBLE_F16) return route_of<F16>(a, stream);
-    return route_of<BF16>(a, stream);
+    if (a.rows.chunks > 0) {
+        const hipError_t e = dtype == NIMBLE_F32   ? route_f32(a, stream)
+                             : dtype == NIMBLE_F16 ? route_f16(a, stream)
+                                                   : route_bf16(a, stream);
+        if (e != hipSuccess || !a.counts) return e;
+    }
+    if (!a.counts) return hipSuccess;
+    k_route_finish<<<dim3(a.rows.segments, (a.experts + kWave - 1) / kWave), kFinishWaves * kWave, 0,
+                     stream>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_balance_loss(int32_t segments, int32_t experts, int32_t top_k,
@@ -793,9 +232,10 @@ hipError_t launch_balance_loss(int32_t segments, int32_t experts, int32_t top_k,
 
 hipError_t launch_route_backward(const BackwardArgs &a, int32_t dtype, hipStream_t stream)
 {
-    if (dtype == NIMBLE_F32) return backward_of<F32>(a, stream);
-    if (dtype == NIMBLE_F16) return backward_of<F16>(a, stream);
-    return backward_of<BF16>(a, stream);
+    if (a.rows.chunks == 0) return hipSuccess;
+    return dtype == NIMBLE_F32   ? backward_f32(a, stream)
+           : dtype == NIMBLE_F16 ? backward_f16(a, stream)
+                                 : backward_bf16(a, stream);
 }
 
 hipError_t launch_counts(const CountArgs &a, hipStream_t stream)

@@ -62,7 +62,7 @@ struct CountArgs {
     int32_t *part;               // [chunks + segments][experts if counts][ranks if rank_tokens]
 };
 
-int32_t route_chunk(int32_t tokens, int32_t experts);
+int32_t route_chunk(int32_t tokens, int32_t experts, bool sums);
 int32_t count_chunk(int32_t tokens, int32_t top_k);
 
 hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream);

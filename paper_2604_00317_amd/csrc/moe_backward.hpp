@@ -1,0 +1,150 @@
+// Gradient of the logits (include/nimble_moe.h).  Rows lie in lanes as in moe_route.hpp.  One pass over the
+// logits: probabilities are made again (a stored sum would save 4 bytes of 2 KB, and lose accuracy for
+// large logits), the choice's part comes through LDS, a float per column of every row at work.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "kernels_moe.hpp"
+#include "moe_device.hpp"
+
+namespace nimble::moe {
+
+namespace {
+
+template <class D, int L, int V>
+__global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArgs a, int shape)
+{
+    constexpr int C = L * V, G = kWave / L;
+    __shared__ __align__(16) float slots[kRowWaves * G][C];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l = lane & (L - 1), g = lane / L;
+    const bool sigmoid = (a.flags & NIMBLE_MOE_SIGMOID) != 0;
+    const bool renorm = (a.flags & NIMBLE_MOE_RENORM) != 0;
+    const float per_scale = 1.0f / a.scale;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
+    const int lo = static_cast<int>(first);
+    const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
+    float *mine = slots[wave * G + g];
+#pragma unroll
+    for (int j = 0; j < V; ++j) mine[column_of<L>(j) + l * kRun] = 0.0f;
+    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
+        if (begin_of(a.rows, s) >= hi) break;
+        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
+        if (from >= to) continue;
+        float coef[V];
+        double unit = 0.0;
+        if (a.counts) {
+            const double n = static_cast<double>(a.routed[s]);
+            if (a.routed[s] != 0)
+                unit = static_cast<double>(a.grad_loss[s]) * static_cast<double>(a.alpha) * a.experts /
+                       (static_cast<double>(a.top_k) * n * n);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int col = column_of<L>(j) + l * kRun;
+            coef[j] = a.counts && col < a.experts
+                          ? static_cast<float>(unit * a.counts[static_cast<int64_t>(s) * a.experts + col])
+                          : 0.0f;
+        }
+        for (int r0 = from + wave * G; r0 < to; r0 += kRowWaves * G) {
+            const bool inside = r0 + g < to;
+            const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
+            const bool kept = !a.keep || a.keep[row] != 0;
+            float x[V];
+            load_row<D, L, V>(static_cast<const typename D::Raw *>(a.logits) + row * a.stride, a.experts, l,
+                              shape, x);
+            int index = -1;
+            float w = 0.0f, wg = 0.0f, gw = 0.0f;
+            bool nan = false;
+            if (kept && l < a.top_k) {
+                index = a.index[row * a.top_k + l];
+                if (static_cast<uint32_t>(index) >= static_cast<uint32_t>(a.experts)) index = -1;
+                w = a.weight[row * a.top_k + l];
+                nan = l == 0 && !(w == w);
+                if (index >= 0 && a.grad_weight) gw = a.grad_weight[row * a.top_k + l];
+                w = index >= 0 ? w : 0.0f;
+                wg = w * gw;
+            }
+            const float all = group_sum<16>(wg);
+            const float slope = w * (gw - (renorm ? all * per_scale : 0.0f));
+            if (index >= 0 && inside) atomicAdd(&mine[index], slope);
+            float top = x[0], sum = 0.0f, rest = 0.0f, r[V];
+#pragma unroll
+            for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
+            top = group_max<L>(top);
+            const Shifted by(shift_of(sigmoid, top));
+            if (sigmoid) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float e = exp_of(-fabsf(x[j]));
+                    r[j] = __builtin_amdgcn_rcpf(1.0f + e) * (x[j] > 0.0f ? e : 1.0f);       // 1 - s
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) r[j] = 1.0f;
+            }
+            scores_of<V>(sigmoid, x, by);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                sum = sum + x[j];
+                rest = __builtin_fmaf(x[j], coef[j], rest);
+            }
+            const float inv = 1.0f / group_sum<L>(sum);
+            rest = group_sum<L>(rest) * inv;
+            // sums over the slots are in the first 16 lanes of a group
+            if (!sigmoid && !renorm) rest = rest + __shfl(all, lane & ~(L - 1));
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int q = 0; q < V / kRun; ++q) {
+                const float4 m = *reinterpret_cast<const float4 *>(&mine[column_of<L>(q * kRun) + l * kRun]);
+                const float v[kRun] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+                for (int i = 0; i < kRun; ++i) {
+                    const int j = q * kRun + i;
+                    x[j] = r[j] * __builtin_fmaf(x[j] * inv, coef[j] - rest, v[i]);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (index >= 0 && inside) mine[index] = 0.0f;
+            // rows that are left out, and rows without a choice
+            const unsigned long long with = __ballot(index >= 0), without = __ballot(nan);
+            const unsigned long long group = (L == kWave ? ~0ull : (1ull << (L & 63)) - 1) << (lane & ~(L - 1));
+            if ((with & group) == 0) {
+                const float fill = (without & group) != 0 ? __builtin_nanf("") : 0.0f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = fill;
+            }
+            if (inside)
+                store_row<D, L, V>(static_cast<typename D::Raw *>(a.grad) + row * a.grad_stride, a.experts, l,
+                                   shape, x);
+        }
+    }
+}
+
+template <class D, int L, int V>
+hipError_t run(const BackwardArgs &a, hipStream_t stream)
+{
+    constexpr size_t B = sizeof(typename D::Raw);
+    const int shape = std::max(shape_of(a.logits, a.stride, a.experts, L * V, B),
+                               shape_of(a.grad, a.grad_stride, a.experts, L * V, B));
+    k_route_backward<D, L, V><<<a.rows.chunks, kRowWaves * kWave, 0, stream>>>(a, shape);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+template <class D>
+hipError_t backward_rows(const BackwardArgs &a, hipStream_t stream)
+{
+    if (a.experts <= 64) return run<D, 16, 4>(a, stream);
+    if (a.experts <= 128) return run<D, 16, 8>(a, stream);
+    if (a.experts <= 256) return run<D, 16, 16>(a, stream);
+    if (a.experts <= 512) return run<D, 32, 16>(a, stream);
+    if (a.experts <= 1024) return run<D, 64, 16>(a, stream);
+    return run<D, 64, 32>(a, stream);
+}
+
+}  // namespace nimble::moe

@@ -1,0 +1,324 @@
+// Device code shared by the routing kernels: element types, reductions over lanes, segments, scores.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "../../include/nimble_moe.h"
+#include "kernels_moe.hpp"
+#include "wave_ops.hpp"
+
+namespace nimble::moe {
+
+namespace {
+
+constexpr float kInf = __builtin_inff();
+constexpr int kRowWaves = 8;         // waves of a workgroup that works on rows
+
+// ---- element types ---------------------------------------------------------------------------
+
+struct F32 {
+    using Raw = float;
+    static constexpr bool kWide = true;      // its bits do not leave room for a column
+    static __device__ __forceinline__ float up(float v) { return v; }
+    static __device__ __forceinline__ float down(float v) { return v; }
+};
+struct F16 {
+    using Raw = uint16_t;
+    static constexpr bool kWide = false;
+    static __device__ __forceinline__ float up(uint16_t v)
+    {
+        return static_cast<float>(__builtin_bit_cast(_Float16, v));
+    }
+    static __device__ __forceinline__ uint16_t down(float v)
+    {
+        return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
+    }
+};
+struct BF16 {
+    using Raw = uint16_t;
+    static constexpr bool kWide = false;
+    static __device__ __forceinline__ float up(uint16_t v)
+    {
+        return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
+    }
+    static __device__ __forceinline__ uint16_t down(float v)
+    {
+        return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+    }
+};
+
+// ---- reductions over lanes -------------------------------------------------------------------
+
+struct TwoI32 {
+    int a, b;
+};
+__device__ __forceinline__ TwoI32 both_rows(int v)           // of a pair of rows of 16 lanes
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return {static_cast<int>(r[0]), static_cast<int>(r[1])};
+}
+__device__ __forceinline__ TwoI32 both_halves(int v)         // of the wave
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return {static_cast<int>(r[0]), static_cast<int>(r[1])};
+}
+__device__ __forceinline__ int bits_of(float v) { return __builtin_bit_cast(int, v); }
+__device__ __forceinline__ float float_of(int v) { return __builtin_bit_cast(float, v); }
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v)
+{
+    return float_of(dpp_i32<CTRL>(bits_of(v)));
+}
+
+// Over aligned groups of L lanes (16, 32 or 64); the same bits in all lanes of a group.
+template <int L>
+__device__ __forceinline__ int group_max(int v)
+{
+    v = max(v, dpp_i32<kDppXor1>(v));
+    v = max(v, dpp_i32<kDppXor2>(v));
+    v = max(v, dpp_i32<kDppHalfMirror>(v));
+    v = max(v, dpp_i32<kDppMirror>(v));
+    if constexpr (L > 16) {
+        const TwoI32 r = both_rows(v);
+        v = max(r.a, r.b);
+    }
+    if constexpr (L > 32) {
+        const TwoI32 h = both_halves(v);
+        v = max(h.a, h.b);
+    }
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v)
+{
+    v = fmaxf(v, dpp_f32<kDppXor1>(v));
+    v = fmaxf(v, dpp_f32<kDppXor2>(v));
+    v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+    v = fmaxf(v, dpp_f32<kDppMirror>(v));
+    if constexpr (L > 16) {
+        const TwoI32 r = both_rows(bits_of(v));
+        v = fmaxf(float_of(r.a), float_of(r.b));
+    }
+    if constexpr (L > 32) {
+        const TwoI32 h = both_halves(bits_of(v));
+        v = fmaxf(float_of(h.a), float_of(h.b));
+    }
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float v)
+{
+    v = v + dpp_f32<kDppXor1>(v);
+    v = v + dpp_f32<kDppXor2>(v);
+    v = v + dpp_f32<kDppHalfMirror>(v);
+    v = v + dpp_f32<kDppMirror>(v);
+    if constexpr (L > 16) {
+        const TwoI32 r = both_rows(bits_of(v));
+        v = float_of(r.a) + float_of(r.b);
+    }
+    if constexpr (L > 32) {
+        const TwoI32 h = both_halves(bits_of(v));
+        v = float_of(h.a) + float_of(h.b);
+    }
+    return v;
+}
+// The sum of a value over the groups of a wave, by lane of a group; the same bits in all groups.
+template <int L>
+__device__ __forceinline__ float over_groups(float v)
+{
+    if constexpr (L < 32) {
+        const TwoI32 r = both_rows(bits_of(v));
+        v = float_of(r.a) + float_of(r.b);
+    }
+    if constexpr (L < 64) {
+        const TwoI32 h = both_halves(bits_of(v));
+        v = float_of(h.a) + float_of(h.b);
+    }
+    return v;
+}
+
+// ---- scores ----------------------------------------------------------------------------------
+
+constexpr float kLog2E = 1.44269504f;
+
+// exp by the hardware's exp2: off by 2^-23 |x| and a step or so, relative; results below 2^-126 are 0
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
+// 1 / (1 + exp(-x)); 0 below -88 or so
+__device__ __forceinline__ float sigmoid_of(float x)
+{
+    return __builtin_amdgcn_rcpf(1.0f + exp_of(-x));
+}
+
+// exp(x - shift) up to a factor that is the same for all x (the rounding of `at`, shift * log2(e)), in a
+// multiply-add and an exp2.  Where `at` is not finite there is no such factor, and far() says so.
+struct Shifted {
+    float shift, at;
+    __device__ __forceinline__ explicit Shifted(float s) : shift(s), at(s * kLog2E) {}
+    __device__ __forceinline__ bool far() const { return fabsf(at) == kInf; }
+    __device__ __forceinline__ float near_exp(float x) const
+    {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2E, -at));
+    }
+    __device__ __forceinline__ float exp(float x) const { return far() ? exp_of(x - shift) : near_exp(x); }
+};
+
+// Scores of a row are summed and compared as s(x) exp(-shift).  Softmax: shift is the largest logit.
+// Sigmoid: 0, unless the largest logit is so low that all sigmoids would vanish in 32 bits; it is
+// that logit then, and s(x) = exp(x).
+__device__ __forceinline__ float shift_of(bool sigmoid, float top)
+{
+    return top == -kInf || (sigmoid && top >= -60.0f) ? 0.0f : top;
+}
+__device__ __forceinline__ float score_of(bool sigmoid, float x, const Shifted &by)
+{
+    const float e = by.exp(x);
+    return sigmoid && by.shift == 0.0f ? sigmoid_of(x) : e;
+}
+// All scores of a row's lane; the choice between forms is the wave's.
+template <int V>
+__device__ __forceinline__ void scores_of(bool sigmoid, float (&x)[V], const Shifted &by)
+{
+    if (__ballot(sigmoid ? by.shift != 0.0f : by.far()) != 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = score_of(sigmoid, x[j], by);
+    } else if (sigmoid) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = sigmoid_of(x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = by.near_exp(x[j]);
+    }
+}
+
+// ---- segments --------------------------------------------------------------------------------
+
+__device__ __forceinline__ int offset(const Rows &r, int s)
+{
+    return min(max(r.seg_ptr[s], 0), r.tokens);
+}
+__device__ __forceinline__ int begin_of(const Rows &r, int s) { return r.seg_ptr ? offset(r, s) : 0; }
+__device__ __forceinline__ int end_of(const Rows &r, int s)
+{
+    return r.seg_ptr ? offset(r, s + 1) : r.tokens;
+}
+
+// The first segment that ends behind `row`, by a search with 64 tries at a time (a round trip to
+// memory each).  All lanes of the wave are active and get the same answer.
+__device__ __forceinline__ int first_segment(const Rows &r, int row, int lane)
+{
+    if (!r.seg_ptr) return 0;
+    int at = 0, n = r.segments;
+    while (n > 0) {
+        const int step = (n + kWave - 1) / kWave;
+        const int s = at + lane * step + step - 1;
+        const bool behind = s >= at + n || r.seg_ptr[s + 1] > row;
+        const unsigned long long hit = __ballot(behind);
+        if (hit == 0) return at + n;
+        const int to = at + (__ffsll(hit) - 1) * step;
+        n = min(step - 1, at + n - to);
+        at = to;
+    }
+    return at;
+}
+
+// ---- rows in lanes ---------------------------------------------------------------------------
+
+// A row lies in a group of L lanes, V values per lane in runs of W neighbours (one load each): lane
+// l of the group has columns q * L W + l W + 0 .. W-1 for q = 0 .. V/W - 1.  A wave holds 64/L rows.
+constexpr int kRun = 4;
+
+template <class D, int W>
+struct alignas(sizeof(typename D::Raw) * W) Run {
+    typename D::Raw v[W];
+};
+
+// Column of value j without the lane's part, l * kRun.
+template <int L>
+constexpr int column_of(int j) { return (j / kRun) * (L * kRun) + j % kRun; }
+
+// The value, but where the compiler cannot see what it depends on: what is worked out from it inside a
+// loop stays there, where a dozen comparisons kept over the loop would take all scalar registers.
+__device__ __forceinline__ int anew(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ int anew_uniform(int v)
+{
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
+// How a row is read and written: kFull, its runs fill the lanes and are aligned to their size; kWhole, it is
+// made of such runs, but does not fill the lanes; kSingle, value by value.
+enum Shape : int { kFull, kWhole, kSingle };
+
+// Columns beyond the row's end come as -inf, like masked ones.  (No read waits for a branch: lanes
+// without a column read one that is there.)
+template <class D, int L, int V>
+__device__ __forceinline__ void load_row(const typename D::Raw *row, int experts, int l, int shape,
+                                         float (&x)[V])
+{
+    const int at = anew(l * kRun);
+    if (shape == kFull) {
+        Run<D, kRun> r[V / kRun];
+#pragma unroll
+        for (int q = 0; q < V / kRun; ++q)
+            r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + q * (L * kRun) + at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = D::up(r[j / kRun].v[j % kRun]);
+    } else if (shape == kWhole) {
+        Run<D, kRun> r[V / kRun];
+#pragma unroll
+        for (int q = 0; q < V / kRun; ++q) {
+            const int col = q * (L * kRun) + at;
+            r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + (col < experts ? col : 0));
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float v = D::up(r[j / kRun].v[j % kRun]);
+            x[j] = (j / kRun) * (L * kRun) + at < experts ? v : -kInf;
+        }
+    } else {
+        typename D::Raw r[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) r[j] = row[min(column_of<L>(j) + at, experts - 1)];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float v = D::up(r[j]);
+            x[j] = column_of<L>(j) + at < experts ? v : -kInf;
+        }
+    }
+}
+
+template <class D, int L, int V>
+__device__ __forceinline__ void store_row(typename D::Raw *row, int experts, int l, int shape,
+                                          const float (&x)[V])
+{
+    const int at = anew(l * kRun);
+    if (shape != kSingle) {
+#pragma unroll
+        for (int q = 0; q < V / kRun; ++q) {
+            const int col = q * (L * kRun) + at;
+            Run<D, kRun> r;
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) r.v[i] = D::down(x[q * kRun + i]);
+            if (col < experts) *reinterpret_cast<Run<D, kRun> *>(row + col) = r;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (column_of<L>(j) + at < experts) row[column_of<L>(j) + at] = D::down(x[j]);
+    }
+}
+
+inline int shape_of(const void *base, int64_t stride, int experts, int columns, size_t bytes)
+{
+    const bool aligned = reinterpret_cast<uintptr_t>(base) % (kRun * bytes) == 0 && stride % kRun == 0;
+    if (!aligned || experts % kRun != 0) return kSingle;
+    return experts == columns ? kFull : kWhole;
+}
+
+}  // namespace
+
+}  // namespace nimble::moe

@@ -1,0 +1,352 @@
+// Choice of experts, their weights, and the sums of the balance loss (include/nimble_moe.h).
+//
+// A row lies in a group of 16 to 64 lanes (moe_device.hpp), so a wave works on up to four rows at a
+// time.  What bounds the kernel is the choice: everything else is a dozen operations per logit.  It
+// is made of minima and maxima of 32-bit whole numbers, without branches:
+//   - a logit becomes a key whose order as a whole number is its order as a float (the bits, with
+//     all but the sign turned round below zero), with the column, turned round, in the lowest
+//     log2(L V) bits: keys are distinct, and among equal values the lower column is the larger key;
+//   - every lane sorts its V keys down to the KL largest (sorting networks of KL keys, then merges
+//     of two lists: the larger ones of one list and the other backwards, sorted again);
+//   - slot after slot, the largest head of all lanes is the next choice, and its lane's list moves up.
+// Keys of 16-bit logits lose nothing: 13 bits of their binary32 form are zero.  Those of binary32
+// logits and of sums with a bias lose their last bits, so one slot more is looked at, and where two
+// neighbours in the order agree in the bits that are left, the wave chooses again by whole values
+// (1 to 5 % of waves with ordinary logits, all of them where most logits are equal).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <climits>
+
+#include "kernels_moe.hpp"
+#include "moe_device.hpp"
+
+namespace nimble::moe {
+
+namespace {
+
+// ---- choice ----------------------------------------------------------------------------------
+
+// The order of floats as an order of whole numbers, and back.
+__device__ __forceinline__ int in_order(int bits) { return bits ^ ((bits >> 31) & 0x7FFFFFFF); }
+
+// The key of a value: its order, with the column's bits in the place of the lowest.
+__device__ __forceinline__ int key_of(float y, int cols, int column)
+{
+    return __builtin_amdgcn_bitop3_b32(in_order(bits_of(y)), cols, column, 0xBA);       // (a & ~b) | c
+}
+
+constexpr int kNoKey = static_cast<int>(0x807FFFFF);     // keys up to this one stand for -inf
+
+__device__ __forceinline__ void order(int &a, int &b)     // the larger one first
+{
+    const int hi = max(a, b), lo = min(a, b);
+    a = hi;
+    b = lo;
+}
+
+// Every place in a list is a constant of the program: keys stay in registers.
+
+// Sorts a[A .. A+N-1], the largest first (odd-even merge sort: runs of P, compared Q apart).
+template <int N, int A, int P = 1, int Q = 1, int S>
+__device__ __forceinline__ void sort_keys(int (&a)[S])
+{
+    if constexpr (P < N) {
+#pragma unroll
+        for (int i = 0; i < N - Q; ++i) {
+            const bool pair = i >= Q % P && (i - Q % P) / Q % 2 == 0 && i / (2 * P) == (i + Q) / (2 * P);
+            if (pair) order(a[A + i], a[A + i + Q]);
+        }
+        if constexpr (Q > 1) sort_keys<N, A, P, Q / 2>(a);
+        else sort_keys<N, A, 2 * P, 2 * P>(a);
+    }
+}
+
+// Sorts a[A .. A+N-1] that rises and then falls, the largest first.
+template <int N, int A, int D = N / 2, int S>
+__device__ __forceinline__ void sort_bitonic(int (&a)[S])
+{
+    if constexpr (D >= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((i & D) == 0) order(a[A + i], a[A + i + D]);
+        sort_bitonic<N, A, D / 2>(a);
+    }
+}
+
+// The N largest keys of a[A .. A+S-1], sorted, in a[A .. A+N-1]: of two sorted halves the larger ones of one
+// list and the other backwards, sorted again.
+template <int N, int A, int M, int S>
+__device__ __forceinline__ void largest(int (&a)[S])
+{
+    if constexpr (M == N) {
+        sort_keys<N, A>(a);
+    } else {
+        largest<N, A, M / 2>(a);
+        largest<N, A + M / 2, M / 2>(a);
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[A + i] = max(a[A + i], a[A + M / 2 + N - 1 - i]);
+        sort_bitonic<N, A>(a);
+    }
+}
+
+struct Choice {
+    int slot;                    // key of the lane's slot; kNoKey or less: there is none
+    int top;                     // the largest key of the row, in all lanes
+    bool unsure;                 // keys do not tell the order
+};
+
+// Slot R: the largest head of all lists in key[0 .. N-1] is taken, and its list moves up.
+template <int L, int V, int KL, int N, int R>
+__device__ __forceinline__ void take(int (&key)[V], int top_k, bool rounded, int l, int mine, int before,
+                                     Choice &c)
+{
+    constexpr int kCols = L * V - 1;
+    if (R > top_k || (R == top_k && !rounded)) return;
+    const int head = key[0] | mine;
+    const int best = group_max<L>(head);
+    if constexpr (R == 0) c.top = best;
+    if constexpr (R > 0) c.unsure = c.unsure || (((best ^ before) & ~kCols) == 0 && best > kNoKey);
+    if (R == top_k) {
+        if constexpr (N < V) c.unsure = c.unsure || key[0] == INT_MIN;   // a list that ends too early
+        return;
+    }
+    if constexpr (R < KL) {
+        c.slot = l == R ? best : c.slot;
+        const bool won = head == best;
+        // (both values are read before one is picked: a pick between two places would make the list memory)
+#pragma unroll
+        for (int i = 0; i + 1 < N; ++i) {
+            const int here = key[i], next = key[i + 1];
+            if (i + R < KL) key[i] = won ? next : here;
+        }
+        if constexpr (N + R <= KL) key[N - 1] = won ? INT_MIN : key[N - 1];
+        take<L, V, KL, N, R + 1>(key, top_k, rounded, l, mine, best, c);
+    }
+}
+
+// The top_k <= KL largest keys of every group, slot j's in lane j.  If `rounded`, keys have lost bits, and
+// one key more is looked at.  The keys are used up.
+template <int L, int V, int KL>
+__device__ __forceinline__ Choice choose(int (&key)[V], int top_k, bool rounded, int l)
+{
+    constexpr int N = V < KL ? V : KL;
+    largest<N, 0, V>(key);
+    Choice c{kNoKey, kNoKey, false};
+    take<L, V, KL, N, 0>(key, top_k, rounded, l, ((L - 1) ^ l) * kRun, 0, c);   // (the lane's part of the columns)
+    return c;
+}
+
+// The same by values y (-inf: not to be chosen): column of slot l, or -1.
+template <int L, int V>
+__device__ __forceinline__ int choose_by_value(float (&y)[V], int top_k, int l)
+{
+    int index = -1;
+    for (int r = 0; r < top_k; ++r) {
+        float best = y[0];
+#pragma unroll
+        for (int j = 1; j < V; ++j) best = fmaxf(best, y[j]);
+        best = group_max<L>(best);
+        int col = INT_MIN;                               // the largest of -1 - column
+#pragma unroll
+        for (int j = 0; j < V; ++j) col = max(col, y[j] == best ? ~(column_of<L>(j) + l * kRun) : INT_MIN);
+        col = ~group_max<L>(col);
+        if (!(best > -kInf)) col = -1;                   // nothing left, or NaN
+        if (l == r) index = col;
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = column_of<L>(j) + l * kRun == col ? -kInf : y[j];
+    }
+    return index;
+}
+
+// ---- rows ------------------------------------------------------------------------------------
+
+// y = x + bias, the keys as floats; without a bias -0 becomes +0, which equals it.
+template <int L, int V>
+__device__ __forceinline__ void add_bias(const RouteArgs &a, int l, const float (&x)[V], float (&y)[V])
+{
+    if (a.bias) {
+        const int at = anew(l * kRun);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            // NaN counts as -inf and +inf as the largest number: the sum with -inf stays -inf
+            float b = a.bias[min(column_of<L>(j) + at, a.experts - 1)];
+            b = b == b ? fminf(b, 3.402823466e38f) : -kInf;
+            y[j] = x[j] + (b + 0.0f);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = x[j] + 0.0f;
+    }
+}
+
+// A workgroup per chunk of rows, cut where a segment ends; probabilities are summed in registers,
+// slots counted in LDS, and the waves' sums added in order at the end of every part.
+template <class D, int L, int V, int KL, bool SUMS>
+__global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int shape)
+{
+    constexpr int C = L * V, G = kWave / L, kCols = C - 1;
+    extern __shared__ float lds[];
+    float *sums = lds;                                   // [kRowWaves][C]
+    int *hits = reinterpret_cast<int *>(lds + kRowWaves * C);
+    int *routed = hits + C;                              // [kRowWaves]
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l = lane & (L - 1), g = lane / L;
+    const bool sigmoid = (a.flags & NIMBLE_MOE_SIGMOID) != 0;
+    const bool renorm = (a.flags & NIMBLE_MOE_RENORM) != 0;
+    const bool rounded = D::kWide || a.bias != nullptr;
+    const float nan = __builtin_nanf("");
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
+    const int lo = static_cast<int>(first);
+    const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
+    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
+        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
+        if (begin_of(a.rows, s) >= hi) break;
+        if (from >= to) continue;
+        if constexpr (SUMS) {
+            for (int c = threadIdx.x; c < C; c += kRowWaves * kWave) hits[c] = 0;
+            __syncthreads();
+        }
+        float acc[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+        int n = 0;
+        for (int r0 = from + wave * G; r0 < to; r0 += kRowWaves * G) {
+            const bool inside = r0 + g < to;
+            const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
+            const bool live = inside && (!a.keep || a.keep[row] != 0);
+            const auto *logits = static_cast<const typename D::Raw *>(a.logits) + row * a.stride;
+            float x[V];
+            load_row<D, L, V>(logits, a.experts, l, shape, x);
+            if (__ballot(live) != ~0ull) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = live ? x[j] : -kInf;
+            }
+            Choice c;
+            int index;
+            {
+                float y[V];
+                int key[V];
+                add_bias<L, V>(a, l, x, y);
+                const int cols = anew(kCols);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    key[j] = key_of(y[j], cols, kCols ^ column_of<L>(j) ^ ((L - 1) * kRun));
+                c = choose<L, V, KL>(key, anew_uniform(a.top_k), rounded, anew(l));
+                index = c.slot > kNoKey ? ~c.slot & kCols : -1;
+                if (rounded && __ballot(c.unsure) != 0) {
+                    add_bias<L, V>(a, l, x, y);
+                    index = choose_by_value<L, V>(y, a.top_k, l);
+                }
+            }
+            const bool chosen = __shfl(index, lane & ~(L - 1)) >= 0;
+            float top, logit;
+            if (rounded) {
+                top = x[0];
+#pragma unroll
+                for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
+                top = group_max<L>(top);
+                logit = index >= 0 ? D::up(logits[index]) : -kInf;
+            } else {
+                top = c.top > kNoKey ? float_of(in_order(c.top) & ~kCols) : -kInf;
+                logit = index >= 0 ? float_of(in_order(c.slot) & ~kCols) : -kInf;
+            }
+            const Shifted by(shift_of(sigmoid, top));
+            scores_of<V>(sigmoid, x, by);
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum = sum + x[j];
+            sum = group_sum<L>(sum);
+            const bool bad = !(sum == sum) || top == kInf;
+            const float inv = __builtin_amdgcn_rcpf(sum);
+            float w;
+            if (renorm) {
+                const float t = group_max<16>(logit);
+                const float u = score_of(sigmoid, logit, Shifted(shift_of(sigmoid, t)));
+                w = u / group_sum<16>(u);
+            } else {
+                w = sigmoid ? sigmoid_of(logit) : by.exp(logit) * inv;
+            }
+            if (bad) index = -1;
+            w = bad ? nan : (index < 0 ? 0.0f : w * a.scale);
+            if (l < a.top_k && inside) {
+                a.index[row * a.top_k + l] = index;
+                a.weight[row * a.top_k + l] = w;
+            }
+            if constexpr (SUMS) {
+                const float of_row = bad ? nan : (chosen ? inv : 0.0f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] = __builtin_fmaf(x[j], of_row, acc[j]);
+                n += chosen && !bad ? 1 : 0;
+                if (l < a.top_k && index >= 0) atomicAdd(&hits[index], 1);
+            }
+        }
+        if constexpr (SUMS) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = over_groups<L>(acc[j]);
+            if (g == 0) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) sums[wave * C + column_of<L>(j) + l * kRun] = acc[j];
+            }
+            int m = 0;
+#pragma unroll
+            for (int i = 0; i < G; ++i) m += __builtin_amdgcn_readlane(n, i * L);
+            if (lane == 0) routed[wave] = m;
+            __syncthreads();
+            const int64_t part = static_cast<int64_t>(blockIdx.x) + s;
+            for (int c = threadIdx.x; c < a.experts; c += kRowWaves * kWave) {
+                float t = sums[c];
+#pragma unroll
+                for (int w = 1; w < kRowWaves; ++w) t = t + sums[w * C + c];
+                a.part_prob[part * a.experts + c] = t;
+                a.part_count[part * a.experts + c] = hits[c];
+            }
+            if (threadIdx.x == 0) {
+                int t = 0;
+                for (int w = 0; w < kRowWaves; ++w) t += routed[w];
+                a.part_routed[part] = t;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+template <class D, int L, int V, int KL>
+hipError_t run(const RouteArgs &a, hipStream_t stream)
+{
+    const int shape = shape_of(a.logits, a.stride, a.experts, L * V, sizeof(typename D::Raw));
+    const dim3 grid(a.rows.chunks), block(kRowWaves * kWave);
+    if (a.counts) {
+        const size_t lds = sizeof(float) * ((kRowWaves + 1) * L * V + kRowWaves);
+        k_route<D, L, V, KL, true><<<grid, block, lds, stream>>>(a, shape);
+    } else {
+        k_route<D, L, V, KL, false><<<grid, block, 0, stream>>>(a, shape);
+    }
+    return hipGetLastError();
+}
+
+template <class D, int L, int V>
+hipError_t run(const RouteArgs &a, hipStream_t stream)
+{
+    // lists of one more than top_k where there are few: a lane that holds all the chosen ones of a row
+    // cannot tell what comes next
+    if (a.top_k <= 3) return run<D, L, V, 4>(a, stream);
+    if (a.top_k <= 8) return run<D, L, V, 8>(a, stream);
+    return run<D, L, V, 16>(a, stream);
+}
+
+}  // namespace
+
+template <class D>
+hipError_t route_rows(const RouteArgs &a, hipStream_t stream)
+{
+    if (a.experts <= 64) return run<D, 16, 4>(a, stream);
+    if (a.experts <= 128) return run<D, 16, 8>(a, stream);
+    if (a.experts <= 256) return run<D, 16, 16>(a, stream);
+    if (a.experts <= 512) return run<D, 32, 16>(a, stream);
+    if (a.experts <= 1024) return run<D, 64, 16>(a, stream);
+    return run<D, 64, 32>(a, stream);
+}
+
+}  // namespace nimble::moe
