@@ -89,60 +89,118 @@ __global__ __launch_bounds__(256) void k_balance_loss(int experts, double unit, 
 
 // ---- counts and demand -----------------------------------------------------------------------
 
+// Counts.  A thread has whole rows; what bounds the kernel is LDS additions to few places: most rows of
+// a skewed router choose the same experts.  So every bin is there `copies` times, side by side in
+// different banks, one for every copies-th lane.  GPUs are not counted slot by slot: their tokens are the
+// slots of their experts, added up at the end, less the slots that go where an earlier slot of the
+// same row goes, which are few.
 constexpr int kCountBlock = 512;
 
-__global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a)
+// Rows a thread reads before it counts them.
+template <int K>
+constexpr int rows_at_once() { return K <= 4 ? 4 : K <= 8 ? 2 : 1; }
+
+template <int K>
+__global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies, int dup_copies, bool aligned)
 {
+    constexpr int N = rows_at_once<K>();
     extern __shared__ int lds[];
-    const int E = a.experts, M = (a.counts ? E : 0) + (a.rank_tokens ? a.ranks : 0);
-    int *bins = lds;                                 // experts, then ranks
-    int *by_rank = bins + (a.counts ? E : 0);
-    int *place = lds + M;
+    const int E = a.experts, R = a.rank_tokens ? a.ranks : 0;
+    int *bins = lds;                                 // [experts][copies]
+    int *dups = bins + E * copies;                   // [ranks][dup_copies]
+    int *totals = dups + R * dup_copies;             // [ranks]
+    int *place = totals + R;                         // [experts]
     const int lane = threadIdx.x & (kWave - 1);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
-    if (a.rank_tokens)
+    const int copy = threadIdx.x & (copies - 1), dup_copy = threadIdx.x & (dup_copies - 1);
+    if (R)
         for (int e = threadIdx.x; e < E; e += kCountBlock) place[e] = a.place[e];
     for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
         if (begin_of(a.rows, s) >= hi) break;
         const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
         if (from >= to) continue;
-        for (int c = threadIdx.x; c < M; c += kCountBlock) bins[c] = 0;
+        for (int c = threadIdx.x; c < E * copies + R * (dup_copies + 1); c += kCountBlock) lds[c] = 0;
         __syncthreads();
-        for (int row = from + threadIdx.x; row < to; row += kCountBlock) {
-            const int32_t *idx = a.index + static_cast<int64_t>(row) * a.top_k;
-            int to_rank[NIMBLE_MOE_MAX_TOP_K];
+        for (int64_t r0 = from + threadIdx.x; r0 < to; r0 += N * kCountBlock) {
+            int idx[N][K];
 #pragma unroll
-            for (int j = 0; j < NIMBLE_MOE_MAX_TOP_K; ++j) {
-                to_rank[j] = -1;
-                if (j < a.top_k) {
-                    const int e = idx[j];
-                    const bool there = static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
-                    if (there && a.counts) atomicAdd(&bins[e], 1);
-                    if (there && a.rank_tokens) {
-                        const int r = place[e];
-                        bool fresh = static_cast<uint32_t>(r) < static_cast<uint32_t>(a.ranks);
+            for (int n = 0; n < N; ++n) {
+                // (a row that is not there is read as the part's last one, and its indices dropped)
+                const int64_t row = r0 + n * kCountBlock;
+                const int32_t *p = a.index + min(row, static_cast<int64_t>(to) - 1) * K;
+                if (K % 4 == 0 && aligned) {
 #pragma unroll
-                        for (int i = 0; i < j; ++i) fresh = fresh && to_rank[i] != r;
-                        if (fresh) {
-                            to_rank[j] = r;
-                            atomicAdd(&by_rank[r], 1);
-                        }
+                    for (int j = 0; j + 3 < K; j += 4) {
+                        const int4 v = *reinterpret_cast<const int4 *>(p + j);
+                        idx[n][j] = v.x;
+                        idx[n][j + 1] = v.y;
+                        idx[n][j + 2] = v.z;
+                        idx[n][j + 3] = v.w;
+                    }
+                } else if (K % 2 == 0 && aligned) {
+#pragma unroll
+                    for (int j = 0; j + 1 < K; j += 2) {
+                        const int2 v = *reinterpret_cast<const int2 *>(p + j);
+                        idx[n][j] = v.x;
+                        idx[n][j + 1] = v.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < K; ++j) idx[n][j] = p[j];
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const bool inside = r0 + n * kCountBlock < to;
+                int to_rank[K];
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    const int e = idx[n][j];
+                    const bool there = inside && static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
+                    if (there) atomicAdd(&bins[e * copies + copy], 1);
+                    if (R) to_rank[j] = place[there ? e : 0];
+                    if (!there) idx[n][j] = -1;
+                }
+                if (R) {
+#pragma unroll
+                    for (int j = 1; j < K; ++j) {
+                        bool again = false;
+#pragma unroll
+                        for (int i = 0; i < j; ++i) again = again || (to_rank[i] == to_rank[j] && idx[n][i] >= 0);
+                        if (again && idx[n][j] >= 0 && static_cast<uint32_t>(to_rank[j]) < static_cast<uint32_t>(R))
+                            atomicAdd(&dups[to_rank[j] * dup_copies + dup_copy], 1);
                     }
                 }
             }
         }
         __syncthreads();
-        const int64_t part = static_cast<int64_t>(blockIdx.x) + s;
-        for (int c = threadIdx.x; c < M; c += kCountBlock) a.part[part * M + c] = bins[c];
+        const int M = (a.counts ? E : 0) + R;
+        int32_t *part = a.part + (static_cast<int64_t>(blockIdx.x) + s) * M;
+        for (int e = threadIdx.x; e < E; e += kCountBlock) {
+            int t = 0;
+            for (int c = 0; c < copies; ++c) t += bins[e * copies + ((c + e) & (copies - 1))];
+            if (a.counts) part[e] = t;
+            if (R && static_cast<uint32_t>(place[e]) < static_cast<uint32_t>(R)) atomicAdd(&totals[place[e]], t);
+        }
+        if (R) {
+            __syncthreads();
+            for (int r = threadIdx.x; r < R; r += kCountBlock) {
+                int t = totals[r];
+                for (int c = 0; c < dup_copies; ++c) t -= dups[r * dup_copies + ((c + r) & (dup_copies - 1))];
+                part[M - R + r] = t;
+            }
+        }
         __syncthreads();
     }
 }
 
-__global__ __launch_bounds__(kFinishWaves *kWave) void k_counts_finish(CountArgs a)
+// The parts of a segment.  WAVES of them are added at a time, 64 columns per workgroup.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES *kWave) void k_counts_finish(CountArgs a)
 {
-    __shared__ int hits[kFinishWaves][kWave];
+    __shared__ int hits[WAVES][kWave];
     const int E = a.counts ? a.experts : 0, M = E + (a.rank_tokens ? a.ranks : 0);
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int s = blockIdx.x;
@@ -152,13 +210,13 @@ __global__ __launch_bounds__(kFinishWaves *kWave) void k_counts_finish(CountArgs
     const int64_t p1 = lo < hi ? static_cast<int64_t>((hi - 1) / a.rows.chunk) + s : p0 - 1;
     int n = 0;
     if (col < M) {
-#pragma unroll 4
-        for (int64_t p = p0 + wave; p <= p1; p += kFinishWaves) n += a.part[p * M + col];
+#pragma unroll 8
+        for (int64_t p = p0 + wave; p <= p1; p += WAVES) n += a.part[p * M + col];
     }
     hits[wave][lane] = n;
     __syncthreads();
     if (wave != 0 || col >= M) return;
-    for (int w = 1; w < kFinishWaves; ++w) n += hits[w][lane];
+    for (int w = 1; w < WAVES; ++w) n += hits[w][lane];
     if (col < E) a.counts[static_cast<int64_t>(s) * E + col] = n;
     else a.rank_tokens[static_cast<int64_t>(s) * a.ranks + col - E] = n;
 }
@@ -238,17 +296,60 @@ hipError_t launch_route_backward(const BackwardArgs &a, int32_t dtype, hipStream
                                  : backward_bf16(a, stream);
 }
 
+namespace {
+
+template <int K>
+hipError_t counts_of(const CountArgs &a, hipStream_t stream)
+{
+    // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
+    // workgroups to a CU at the largest sizes
+    int copies = 32, dup_copies = 8;
+    while (copies > 1 && a.experts * copies > 8192) copies /= 2;
+    while (dup_copies > 1 && a.ranks * dup_copies > 2048) dup_copies /= 2;
+    const int R = a.rank_tokens ? a.ranks : 0;
+    const size_t lds = sizeof(int) * (static_cast<size_t>(a.experts) * (copies + 1) + R * (dup_copies + 1));
+    const bool aligned = reinterpret_cast<uintptr_t>(a.index) % 16 == 0;
+    k_counts<K><<<a.rows.chunks, kCountBlock, lds, stream>>>(a, copies, dup_copies, aligned);
+    return hipGetLastError();
+}
+
+hipError_t counts_by_top_k(const CountArgs &a, hipStream_t stream)
+{
+    switch (a.top_k) {
+    case 1: return counts_of<1>(a, stream);
+    case 2: return counts_of<2>(a, stream);
+    case 3: return counts_of<3>(a, stream);
+    case 4: return counts_of<4>(a, stream);
+    case 5: return counts_of<5>(a, stream);
+    case 6: return counts_of<6>(a, stream);
+    case 7: return counts_of<7>(a, stream);
+    case 8: return counts_of<8>(a, stream);
+    case 9: return counts_of<9>(a, stream);
+    case 10: return counts_of<10>(a, stream);
+    case 11: return counts_of<11>(a, stream);
+    case 12: return counts_of<12>(a, stream);
+    case 13: return counts_of<13>(a, stream);
+    case 14: return counts_of<14>(a, stream);
+    case 15: return counts_of<15>(a, stream);
+    default: return counts_of<16>(a, stream);
+    }
+}
+
+}  // namespace
+
 hipError_t launch_counts(const CountArgs &a, hipStream_t stream)
 {
-    const int M = (a.counts ? a.experts : 0) + (a.rank_tokens ? a.ranks : 0);
-    const size_t lds = sizeof(int) * (static_cast<size_t>(M) + (a.rank_tokens ? a.experts : 0));
     if (a.rows.chunks > 0) {
-        k_counts<<<a.rows.chunks, kCountBlock, lds, stream>>>(a);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = counts_by_top_k(a, stream);
         if (e != hipSuccess) return e;
     }
-    k_counts_finish<<<dim3(a.rows.segments, (M + kWave - 1) / kWave), kFinishWaves * kWave, 0,
-                      stream>>>(a);
+    const int M = (a.counts ? a.experts : 0) + (a.rank_tokens ? a.ranks : 0);
+    const dim3 grid(a.rows.segments, (M + kWave - 1) / kWave);
+    // a segment has about chunks / segments parts: few are added by one wave, many by sixteen
+    if (a.rows.chunks > 8 * static_cast<int64_t>(a.rows.segments))
+        k_counts_finish<16><<<grid, 16 * kWave, 0, stream>>>(a);
+    else
+        k_counts_finish<1><<<grid, kWave, 0, stream>>>(a);
     return hipGetLastError();
 }
 
