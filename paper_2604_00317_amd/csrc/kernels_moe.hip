@@ -19,50 +19,71 @@ hipError_t backward_bf16(const BackwardArgs &a, hipStream_t stream);
 
 namespace {
 
-constexpr int kFinishWaves = 16;
+// ---- end of the sums -------------------------------------------------------------------------
 
-// The parts of a segment, 64 columns per workgroup: every wave adds each 16th part, in double.
-__global__ __launch_bounds__(kFinishWaves *kWave) void k_route_finish(RouteArgs a)
+// The parts of segment s are p0 .. p1 (none: p1 < p0).
+struct Parts {
+    int64_t p0, p1;
+    __device__ __forceinline__ Parts(const Rows &r, int s)
+    {
+        const int lo = r.seg_ptr ? min(max(r.seg_ptr[s], 0), r.tokens) : 0;
+        const int hi = r.seg_ptr ? min(max(r.seg_ptr[s + 1], 0), r.tokens) : r.tokens;
+        p0 = static_cast<int64_t>(lo / r.chunk) + s;
+        p1 = lo < hi ? static_cast<int64_t>((hi - 1) / r.chunk) + s : p0 - 1;
+    }
+};
+
+// Parts are added by the threads of a workgroup in COLS columns and 1024 / COLS (or one) rows: every row
+// adds each rows-th part, and the first one the rows' sums in order.  What bounds these kernels is the time
+// of a few dependent reads, so many parts (of few segments) take many rows and few columns, and few parts
+// one row and a workgroup of one wave.
+template <int COLS, int ROWS>
+__global__ __launch_bounds__(COLS *ROWS) void k_route_finish(RouteArgs a)
 {
-    __shared__ double sums[kFinishWaves][kWave];
-    __shared__ int hits[kFinishWaves][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int s = blockIdx.x;
-    const int col = blockIdx.y * kWave + lane;
-    const int lo = begin_of(a.rows, s), hi = end_of(a.rows, s);
-    const int64_t p0 = static_cast<int64_t>(lo / a.rows.chunk) + s;
-    const int64_t p1 = lo < hi ? static_cast<int64_t>((hi - 1) / a.rows.chunk) + s : p0 - 1;
+    __shared__ double sums[ROWS][COLS];
+    __shared__ int hits[ROWS][COLS];
+    const int x = threadIdx.x % COLS, y = threadIdx.x / COLS;
+    const int64_t s = blockIdx.x;
+    const int col = blockIdx.y * COLS + x;
+    const Parts parts(a.rows, blockIdx.x);
     double t = 0.0;
     int n = 0;
     if (col < a.experts) {
-#pragma unroll 4
-        for (int64_t p = p0 + wave; p <= p1; p += kFinishWaves) {
+#pragma unroll 8
+        for (int64_t p = parts.p0 + y; p <= parts.p1; p += ROWS) {
             t = t + static_cast<double>(a.part_prob[p * a.experts + col]);
             n += a.part_count[p * a.experts + col];
         }
     }
-    sums[wave][lane] = t;
-    hits[wave][lane] = n;
-    __syncthreads();
-    if (wave == 0 && col < a.experts) {
-        for (int w = 1; w < kFinishWaves; ++w) {
-            t = t + sums[w][lane];
-            n += hits[w][lane];
+    int m = 0;                                       // rows with a choice, by the first columns' workgroup
+    if (blockIdx.y == 0)
+        for (int64_t p = parts.p0 + threadIdx.x; p <= parts.p1; p += COLS * ROWS) m += a.part_routed[p];
+    if constexpr (ROWS > 1) {
+        sums[y][x] = t;
+        hits[y][x] = n;
+        __syncthreads();
+        if (y == 0) {
+            for (int i = 1; i < ROWS; ++i) {
+                t = t + sums[i][x];
+                n += hits[i][x];
+            }
         }
-        a.prob_sum[static_cast<int64_t>(s) * a.experts + col] = static_cast<float>(t);
-        a.counts[static_cast<int64_t>(s) * a.experts + col] = n;
+    }
+    if (y == 0 && col < a.experts) {
+        a.prob_sum[s * a.experts + col] = static_cast<float>(t);
+        a.counts[s * a.experts + col] = n;
     }
     if (blockIdx.y == 0) {
-        int m = 0;
-        for (int64_t p = p0 + threadIdx.x; p <= p1; p += kFinishWaves * kWave) m += a.part_routed[p];
-        __syncthreads();
-        hits[wave][lane] = m;
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < kFinishWaves; ++w) m += hits[w][lane];
-            for (int step = 1; step < kWave; step *= 2) m += __shfl_xor(m, step, kWave);
-            if (lane == 0) a.routed[s] = m;
+        for (int step = 1; step < kWave; step *= 2) m += __shfl_xor(m, step, kWave);
+        if constexpr (ROWS > 1) {
+            __syncthreads();
+            int *each = &hits[0][0];
+            if (threadIdx.x % kWave == 0) each[threadIdx.x / kWave] = m;
+            __syncthreads();
+            m = 0;
+            for (int i = 0; i < COLS * ROWS / kWave; ++i) m += each[i];
         }
+        if (threadIdx.x == 0) a.routed[s] = m;
     }
 }
 
@@ -117,16 +138,19 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies,
     const int copy = threadIdx.x & (copies - 1), dup_copy = threadIdx.x & (dup_copies - 1);
     if (R)
         for (int e = threadIdx.x; e < E; e += kCountBlock) place[e] = a.place[e];
-    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
-        if (begin_of(a.rows, s) >= hi) break;
-        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
+    Segments segments(a.rows, lane);
+    for (int s = segments.first(lo); s < a.rows.segments; ++s) {
+        const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
+        if (begin >= hi) break;
         if (from >= to) continue;
         for (int c = threadIdx.x; c < E * copies + R * (dup_copies + 1); c += kCountBlock) lds[c] = 0;
         __syncthreads();
-        for (int64_t r0 = from + threadIdx.x; r0 < to; r0 += N * kCountBlock) {
+        for (int64_t u0 = from; u0 < to; u0 += N * kCountBlock) {
+            const int64_t r0 = u0 + threadIdx.x;
             int idx[N][K];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
+                if (u0 + n * kCountBlock >= to) break;
                 // (a row that is not there is read as the part's last one, and its indices dropped)
                 const int64_t row = r0 + n * kCountBlock;
                 const int32_t *p = a.index + min(row, static_cast<int64_t>(to) - 1) * K;
@@ -153,6 +177,7 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies,
             }
 #pragma unroll
             for (int n = 0; n < N; ++n) {
+                if (u0 + n * kCountBlock >= to) break;
                 const bool inside = r0 + n * kCountBlock < to;
                 int to_rank[K];
 #pragma unroll
@@ -196,29 +221,30 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies,
     }
 }
 
-// The parts of a segment.  WAVES of them are added at a time, 64 columns per workgroup.
-template <int WAVES>
-__global__ __launch_bounds__(WAVES *kWave) void k_counts_finish(CountArgs a)
+// The parts of a segment, as in k_route_finish.
+template <int COLS, int ROWS>
+__global__ __launch_bounds__(COLS *ROWS) void k_counts_finish(CountArgs a)
 {
-    __shared__ int hits[WAVES][kWave];
+    __shared__ int hits[ROWS][COLS];
     const int E = a.counts ? a.experts : 0, M = E + (a.rank_tokens ? a.ranks : 0);
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int s = blockIdx.x;
-    const int col = blockIdx.y * kWave + lane;
-    const int lo = begin_of(a.rows, s), hi = end_of(a.rows, s);
-    const int64_t p0 = static_cast<int64_t>(lo / a.rows.chunk) + s;
-    const int64_t p1 = lo < hi ? static_cast<int64_t>((hi - 1) / a.rows.chunk) + s : p0 - 1;
+    const int x = threadIdx.x % COLS, y = threadIdx.x / COLS;
+    const int64_t s = blockIdx.x;
+    const int col = blockIdx.y * COLS + x;
+    const Parts parts(a.rows, blockIdx.x);
     int n = 0;
     if (col < M) {
 #pragma unroll 8
-        for (int64_t p = p0 + wave; p <= p1; p += WAVES) n += a.part[p * M + col];
+        for (int64_t p = parts.p0 + y; p <= parts.p1; p += ROWS) n += a.part[p * M + col];
     }
-    hits[wave][lane] = n;
-    __syncthreads();
-    if (wave != 0 || col >= M) return;
-    for (int w = 1; w < WAVES; ++w) n += hits[w][lane];
-    if (col < E) a.counts[static_cast<int64_t>(s) * E + col] = n;
-    else a.rank_tokens[static_cast<int64_t>(s) * a.ranks + col - E] = n;
+    if constexpr (ROWS > 1) {
+        hits[y][x] = n;
+        __syncthreads();
+        if (y == 0)
+            for (int i = 1; i < ROWS; ++i) n += hits[i][x];
+    }
+    if (y != 0 || col >= M) return;
+    if (col < E) a.counts[s * E + col] = n;
+    else a.rank_tokens[s * a.ranks + col - E] = n;
 }
 
 __global__ __launch_bounds__(256) void k_traffic(int64_t total, int ranks, const int32_t *tokens,
@@ -250,20 +276,28 @@ __global__ __launch_bounds__(256) void k_traffic(int64_t total, int ranks, const
 
 }  // namespace
 
-// Whole passes of a workgroup's rows, and no more than 1024 chunks with sums to add up: about four
-// workgroups per CU.
-int32_t route_chunk(int32_t tokens, int32_t experts, bool sums)
+namespace {
+
+int32_t round_up(int64_t rows, int32_t pass)
 {
-    const int32_t pass = kRowWaves * (experts <= 256 ? 4 : experts <= 512 ? 2 : 1);
-    const int32_t most = sums ? 1 << 10 : 1 << 20;
-    const int64_t rows = (static_cast<int64_t>(tokens) + most - 1) / most;
     return static_cast<int32_t>((std::max<int64_t>(rows, 1) + pass - 1) / pass * pass);
 }
 
-int32_t count_chunk(int32_t tokens, int32_t)
+// A segment has about chunks / segments parts.
+bool many_parts(const Rows &r) { return r.chunks > 8 * static_cast<int64_t>(r.segments); }
+
+}  // namespace
+
+// Whole passes of a workgroup's rows; with sums no more than 512 chunks, two workgroups per CU, all
+// of them at work at once.
+int32_t route_chunk(int32_t tokens, int32_t experts, bool sums)
 {
-    return std::max(kCountBlock, (tokens + 1023) / 1024);
+    const int32_t most = sums ? 1 << 9 : 1 << 20;
+    return round_up((static_cast<int64_t>(tokens) + most - 1) / most,
+                    kRowWaves * (experts <= 256 ? 4 : experts <= 512 ? 2 : 1));
 }
+
+int32_t count_chunk(int32_t tokens, int32_t) { return round_up((static_cast<int64_t>(tokens) + 1023) / 1024, kCountBlock); }
 
 hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream)
 {
@@ -274,8 +308,10 @@ hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream)
         if (e != hipSuccess || !a.counts) return e;
     }
     if (!a.counts) return hipSuccess;
-    k_route_finish<<<dim3(a.rows.segments, (a.experts + kWave - 1) / kWave), kFinishWaves * kWave, 0,
-                     stream>>>(a);
+    if (many_parts(a.rows))
+        k_route_finish<16, 64><<<dim3(a.rows.segments, (a.experts + 15) / 16), 1024, 0, stream>>>(a);
+    else
+        k_route_finish<64, 1><<<dim3(a.rows.segments, (a.experts + 63) / 64), 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -302,9 +338,10 @@ template <int K>
 hipError_t counts_of(const CountArgs &a, hipStream_t stream)
 {
     // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
-    // workgroups to a CU at the largest sizes
+    // workgroups to a CU at the largest sizes; and no more bins than a chunk has slots
     int copies = 32, dup_copies = 8;
-    while (copies > 1 && a.experts * copies > 8192) copies /= 2;
+    const int64_t slots = std::min<int64_t>(static_cast<int64_t>(a.rows.chunk) * K, 8192);
+    while (copies > 1 && a.experts * copies > slots) copies /= 2;
     while (dup_copies > 1 && a.ranks * dup_copies > 2048) dup_copies /= 2;
     const int R = a.rank_tokens ? a.ranks : 0;
     const size_t lds = sizeof(int) * (static_cast<size_t>(a.experts) * (copies + 1) + R * (dup_copies + 1));
@@ -344,12 +381,10 @@ hipError_t launch_counts(const CountArgs &a, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     const int M = (a.counts ? a.experts : 0) + (a.rank_tokens ? a.ranks : 0);
-    const dim3 grid(a.rows.segments, (M + kWave - 1) / kWave);
-    // a segment has about chunks / segments parts: few are added by one wave, many by sixteen
-    if (a.rows.chunks > 8 * static_cast<int64_t>(a.rows.segments))
-        k_counts_finish<16><<<grid, 16 * kWave, 0, stream>>>(a);
+    if (many_parts(a.rows))
+        k_counts_finish<16, 64><<<dim3(a.rows.segments, (M + 15) / 16), 1024, 0, stream>>>(a);
     else
-        k_counts_finish<1><<<grid, kWave, 0, stream>>>(a);
+        k_counts_finish<64, 1><<<dim3(a.rows.segments, (M + 63) / 64), 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -30,9 +30,10 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
     float *mine = slots[wave * G + g];
 #pragma unroll
     for (int j = 0; j < V; ++j) mine[column_of<L>(j) + l * kRun] = 0.0f;
-    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
-        if (begin_of(a.rows, s) >= hi) break;
-        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
+    Segments segments(a.rows, lane);
+    for (int s = segments.first(lo); s < a.rows.segments; ++s) {
+        const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
+        if (begin >= hi) break;
         if (from >= to) continue;
         float coef[V];
         double unit = 0.0;

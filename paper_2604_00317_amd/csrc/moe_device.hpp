@@ -192,34 +192,52 @@ __device__ __forceinline__ void scores_of(bool sigmoid, float (&x)[V], const Shi
 
 // ---- segments --------------------------------------------------------------------------------
 
-__device__ __forceinline__ int offset(const Rows &r, int s)
-{
-    return min(max(r.seg_ptr[s], 0), r.tokens);
-}
-__device__ __forceinline__ int begin_of(const Rows &r, int s) { return r.seg_ptr ? offset(r, s) : 0; }
-__device__ __forceinline__ int end_of(const Rows &r, int s)
-{
-    return r.seg_ptr ? offset(r, s + 1) : r.tokens;
-}
+// The segments' offsets, 64 of them at a time in the lanes of a wave: one round trip to memory finds the
+// segment of a row and its ends where there are up to 63 segments.  All lanes are active in every call, and
+// all waves of a workgroup get the same answers.
+class Segments {
+public:
+    __device__ __forceinline__ Segments(const Rows &rows, int lane) : r(rows), lane(lane) {}
 
-// The first segment that ends behind `row`, by a search with 64 tries at a time (a round trip to
-// memory each).  All lanes of the wave are active and get the same answer.
-__device__ __forceinline__ int first_segment(const Rows &r, int row, int lane)
-{
-    if (!r.seg_ptr) return 0;
-    int at = 0, n = r.segments;
-    while (n > 0) {
-        const int step = (n + kWave - 1) / kWave;
-        const int s = at + lane * step + step - 1;
-        const bool behind = s >= at + n || r.seg_ptr[s + 1] > row;
-        const unsigned long long hit = __ballot(behind);
-        if (hit == 0) return at + n;
-        const int to = at + (__ffsll(hit) - 1) * step;
-        n = min(step - 1, at + n - to);
-        at = to;
+    // The first segment that ends behind `row` (the number of segments, if none does).
+    __device__ __forceinline__ int first(int row)
+    {
+        if (!r.seg_ptr) return 0;
+        if (r.segments >= kWave) {                   // 64 tries at a time
+            int at = 0, n = r.segments;
+            while (n > 0) {
+                const int step = (n + kWave - 1) / kWave;
+                const int s = at + lane * step + step - 1;
+                const unsigned long long hit = __ballot(s >= at + n || r.seg_ptr[s + 1] > row);
+                if (hit == 0) return at + n;
+                const int to = at + (__ffsll(hit) - 1) * step;
+                n = min(step - 1, at + n - to);
+                at = to;
+            }
+            fetch(at);
+            return at;
+        }
+        fetch(0);
+        const unsigned long long hit = __ballot(lane >= 1 && lane <= r.segments && offsets > row);
+        return hit == 0 ? r.segments : __ffsll(hit) - 2;
     }
-    return at;
-}
+    __device__ __forceinline__ int begin(int s) { return r.seg_ptr ? offset(s) : 0; }
+    __device__ __forceinline__ int end(int s) { return r.seg_ptr ? offset(s + 1) : r.tokens; }
+
+private:
+    __device__ __forceinline__ void fetch(int s)
+    {
+        base = s;
+        offsets = min(max(r.seg_ptr[min(s + lane, r.segments)], 0), r.tokens);
+    }
+    __device__ __forceinline__ int offset(int s)
+    {
+        if (s - base >= kWave) fetch(s - 1);
+        return __builtin_amdgcn_readlane(offsets, s - base);
+    }
+    const Rows &r;
+    int lane, base = 0, offsets = 0;
+};
 
 // ---- rows in lanes ---------------------------------------------------------------------------
 

@@ -200,9 +200,10 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
-    for (int s = first_segment(a.rows, lo, lane); s < a.rows.segments; ++s) {
-        const int from = max(lo, begin_of(a.rows, s)), to = min(hi, end_of(a.rows, s));
-        if (begin_of(a.rows, s) >= hi) break;
+    Segments segments(a.rows, lane);
+    for (int s = segments.first(lo); s < a.rows.segments; ++s) {
+        const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
+        if (begin >= hi) break;
         if (from >= to) continue;
         if constexpr (SUMS) {
             for (int c = threadIdx.x; c < C; c += kRowWaves * kWave) hits[c] = 0;
