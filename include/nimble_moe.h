@@ -69,7 +69,7 @@ enum { NIMBLE_MOE_WAY_BACK = 1u /* the demand of the way back: destination to so
  *   choice   key_e = x_e + bias_e in binary32 (the bias steers the choice alone: weights,
  *            probabilities and gradients are those of x).  The top_k experts with the largest
  *            keys, largest first, ties to the lower index.  Experts with x = -inf (a mask) or
- *            key = -inf or NaN are not chosen; slots they leave empty, and rows they leave
+ *            key = -inf are not chosen; slots they leave empty, and rows they leave
  *            without a choice, have index -1 and weight 0.  A row that holds NaN or +inf has
  *            no choice either: its indices are -1, its weights NaN, and so are the probability
  *            sums of its segment and the row of the gradient.
@@ -82,7 +82,7 @@ enum { NIMBLE_MOE_WAY_BACK = 1u /* the demand of the way back: destination to so
  *   top_k        1 <= top_k <= min(experts, 16)
  *   dtype        NIMBLE_F32, NIMBLE_F16 or NIMBLE_BF16
  *   d_logits     [tokens][experts], rows row_stride >= experts elements apart
- *   d_bias       float [experts], or NULL
+ *   d_bias       float [experts], or NULL; NaN counts as -inf, +inf as the largest finite number
  *   d_keep       [tokens], 0 for rows to leave out (padding): they have no choice and may hold
  *                anything; or NULL
  *   scale        finite and > 0

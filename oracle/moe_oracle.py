@@ -19,7 +19,11 @@ def log_score(x, sigmoid):
 
 def choose(x32, bias32, top_k):
     """Columns of the top_k largest keys of one row, largest first, ties to the lower one."""
-    key = x32 + bias32 if bias32 is not None else x32 + np.float32(0)
+    if bias32 is None:
+        bias32 = np.float32(0)
+    else:                                     # NaN counts as -inf, +inf as the largest number
+        bias32 = np.minimum(np.where(np.isnan(bias32), -np.inf, bias32), np.finfo(np.float32).max).astype(np.float32)
+    key = x32 + bias32
     ok = [e for e in range(len(x32)) if x32[e] != -np.inf and key[e] > -np.inf]
     return sorted(ok, key=lambda e: (-key[e], e))[:top_k]
 

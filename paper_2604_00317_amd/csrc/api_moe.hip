@@ -120,6 +120,7 @@ nimble_status_t nimble_moe_route(int32_t tokens, int32_t experts, int32_t top_k,
     a.logits = d_logits;
     a.stride = row_stride;
     a.bias = d_bias;
+    a.bias_runs = reinterpret_cast<uintptr_t>(d_bias) % 16 == 0 && experts % 4 == 0;
     a.keep = d_keep;
     a.scale = scale;
     a.index = d_index;

@@ -26,6 +26,7 @@ struct RouteArgs {
     const void *logits;
     int64_t stride;              // in elements
     const float *bias;
+    bool bias_runs;              // it is made of runs of four, aligned to their size
     const uint8_t *keep;
     float scale;
     int32_t *index;

@@ -54,9 +54,8 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             const bool inside = r0 + g < to;
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
             const bool kept = !a.keep || a.keep[row] != 0;
-            float x[V];
-            load_row<D, L, V>(static_cast<const typename D::Raw *>(a.logits) + row * a.stride, a.experts, l,
-                              shape, x);
+            RowOf<D, L, V> raw;
+            raw.load(static_cast<const typename D::Raw *>(a.logits) + row * a.stride, a.experts, l, shape);
             int index = -1;
             float w = 0.0f, wg = 0.0f, gw = 0.0f;
             bool nan = false;
@@ -72,7 +71,9 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             const float all = group_sum<16>(wg);
             const float slope = w * (gw - (renorm ? all * per_scale : 0.0f));
             if (index >= 0 && inside) atomicAdd(&mine[index], slope);
-            float top = x[0], sum = 0.0f, rest = 0.0f, r[V];
+            float x[V], sum = 0.0f, rest = 0.0f, r[V];
+            raw.values(x);
+            float top = x[0];
 #pragma unroll
             for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
             top = group_max<L>(top);

@@ -24,6 +24,7 @@ struct F32 {
 struct F16 {
     using Raw = uint16_t;
     static constexpr bool kWide = false;
+    static constexpr int kInfBits = 0x7C00;
     static __device__ __forceinline__ float up(uint16_t v)
     {
         return static_cast<float>(__builtin_bit_cast(_Float16, v));
@@ -36,6 +37,7 @@ struct F16 {
 struct BF16 {
     using Raw = uint16_t;
     static constexpr bool kWide = false;
+    static constexpr int kInfBits = 0x7F80;
     static __device__ __forceinline__ float up(uint16_t v)
     {
         return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
@@ -271,43 +273,90 @@ __device__ __forceinline__ int anew_uniform(int v)
 // made of such runs, but does not fill the lanes; kSingle, value by value.
 enum Shape : int { kFull, kWhole, kSingle };
 
-// Columns beyond the row's end come as -inf, like masked ones.  (No read waits for a branch: lanes
-// without a column read one that is there.)
+// A row's values as they are read: binary32 one by one, 16-bit ones in pairs.  Columns beyond the row's end
+// come as -inf, like masked ones.  (No read waits for a branch: lanes without a column read one that is there.)
 template <class D, int L, int V>
-__device__ __forceinline__ void load_row(const typename D::Raw *row, int experts, int l, int shape,
-                                         float (&x)[V])
-{
-    const int at = anew(l * kRun);
-    if (shape == kFull) {
-        Run<D, kRun> r[V / kRun];
+struct RowOf {
+    static constexpr int kPer = D::kWide ? 1 : 2;            // values of a word
+    static constexpr int kWords = V / kPer;
+    uint32_t word[kWords];
+
+    static constexpr uint32_t none()
+    {
+        if constexpr (D::kWide) return 0xFF800000u;
+        else return (0x8000u | D::kInfBits) * 0x10001u;
+    }
+    __device__ __forceinline__ void load(const typename D::Raw *row, int experts, int l, int shape)
+    {
+        constexpr int kWordsOfRun = kRun / kPer;
+        const int at = anew(l * kRun);
+        if (shape == kFull) {
 #pragma unroll
-        for (int q = 0; q < V / kRun; ++q)
-            r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + q * (L * kRun) + at);
+            for (int q = 0; q < V / kRun; ++q)
+                put(q, *reinterpret_cast<const Run<D, kRun> *>(row + q * (L * kRun) + at));
+        } else if (shape == kWhole) {
+            Run<D, kRun> r[V / kRun];
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = D::up(r[j / kRun].v[j % kRun]);
-    } else if (shape == kWhole) {
-        Run<D, kRun> r[V / kRun];
+            for (int q = 0; q < V / kRun; ++q) {
+                const int col = q * (L * kRun) + at;
+                r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + (col < experts ? col : 0));
+            }
 #pragma unroll
-        for (int q = 0; q < V / kRun; ++q) {
-            const int col = q * (L * kRun) + at;
-            r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + (col < experts ? col : 0));
-        }
+            for (int q = 0; q < V / kRun; ++q) {
+                put(q, r[q]);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float v = D::up(r[j / kRun].v[j % kRun]);
-            x[j] = (j / kRun) * (L * kRun) + at < experts ? v : -kInf;
-        }
-    } else {
-        typename D::Raw r[V];
+                for (int i = 0; i < kWordsOfRun; ++i) {
+                    const uint32_t w = word[q * kWordsOfRun + i];
+                    word[q * kWordsOfRun + i] = q * (L * kRun) + at < experts ? w : none();
+                }
+            }
+        } else {
+            typename D::Raw r[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) r[j] = row[min(column_of<L>(j) + at, experts - 1)];
+            for (int j = 0; j < V; ++j) r[j] = row[min(column_of<L>(j) + at, experts - 1)];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float v = D::up(r[j]);
-            x[j] = column_of<L>(j) + at < experts ? v : -kInf;
+            for (int w = 0; w < kWords; ++w) {
+                uint32_t v;
+                if constexpr (D::kWide) {
+                    v = static_cast<uint32_t>(bits_of(r[w]));
+                    v = column_of<L>(w) + at < experts ? v : none();
+                } else {
+                    const uint32_t a = r[2 * w], b = r[2 * w + 1], no = none() & 0xFFFFu;
+                    v = (column_of<L>(2 * w) + at < experts ? a : no) |
+                        (column_of<L>(2 * w + 1) + at < experts ? b : no) << 16;
+                }
+                word[w] = v;
+            }
         }
     }
-}
+    __device__ __forceinline__ void drop(bool keep)
+    {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) word[w] = keep ? word[w] : none();
+    }
+    __device__ __forceinline__ float value(int j) const
+    {
+        if constexpr (D::kWide) return float_of(static_cast<int>(word[j]));
+        else return D::up(static_cast<uint16_t>(word[j / 2] >> (j % 2 * 16)));
+    }
+    __device__ __forceinline__ void values(float (&x)[V]) const
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = value(j);
+    }
+
+private:
+    __device__ __forceinline__ void put(int q, const Run<D, kRun> &r)
+    {
+        constexpr int kWordsOfRun = kRun / kPer;
+        struct Words {
+            uint32_t w[kWordsOfRun];
+        };
+        const Words words = __builtin_bit_cast(Words, r);
+#pragma unroll
+        for (int i = 0; i < kWordsOfRun; ++i) word[q * kWordsOfRun + i] = words.w[i];
+    }
+};
 
 template <class D, int L, int V>
 __device__ __forceinline__ void store_row(typename D::Raw *row, int experts, int l, int shape,

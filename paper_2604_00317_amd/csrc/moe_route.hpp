@@ -1,18 +1,17 @@
 // Choice of experts, their weights, and the sums of the balance loss (include/nimble_moe.h).
 //
 // A row lies in a group of 16 to 64 lanes (moe_device.hpp), so a wave works on up to four rows at a
-// time.  What bounds the kernel is the choice: everything else is a dozen operations per logit.  It
+// time.  What bounds the kernel is the choice: everything else is half a dozen operations per logit.  It
 // is made of minima and maxima of 32-bit whole numbers, without branches:
-//   - a logit becomes a key whose order as a whole number is its order as a float (the bits, with
-//     all but the sign turned round below zero), with the column, turned round, in the lowest
-//     log2(L V) bits: keys are distinct, and among equal values the lower column is the larger key;
+//   - a logit becomes a key whose order as a whole number is its order as a float, with the column, turned
+//     round, in the lowest bits: keys are distinct, and among equal values the lower column is the larger;
 //   - every lane sorts its V keys down to the KL largest (sorting networks of KL keys, then merges
 //     of two lists: the larger ones of one list and the other backwards, sorted again);
 //   - slot after slot, the largest head of all lanes is the next choice, and its lane's list moves up.
-// Keys of 16-bit logits lose nothing: 13 bits of their binary32 form are zero.  Those of binary32
-// logits and of sums with a bias lose their last bits, so one slot more is looked at, and where two
-// neighbours in the order agree in the bits that are left, the wave chooses again by whole values
-// (1 to 5 % of waves with ordinary logits, all of them where most logits are equal).
+// A 16-bit logit and its column fit a key.  Binary32 logits, and sums with a bias, lose their last bits to
+// the column (ROUNDED), so one slot more is looked at: where neighbours in the order agree in the bits that are
+// left, the chosen are put in order by whole values, and where that happens at the last one, the wave
+// chooses again by whole values (some 1 % of waves with ordinary logits, all where most are equal).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -27,8 +26,20 @@ namespace {
 
 // ---- choice ----------------------------------------------------------------------------------
 
-// The order of floats as an order of whole numbers, and back.
+// The order of binary32 numbers as an order of whole numbers (of +0 and -0 the first is larger).
 __device__ __forceinline__ int in_order(int bits) { return bits ^ ((bits >> 31) & 0x7FFFFFFF); }
+
+// The order of two 16-bit numbers, in the halves of a word: sign and magnitude as a number (0 is 0), and back.
+typedef short Pair __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ Pair pair_in_order(uint32_t w)
+{
+    const Pair sign = __builtin_bit_cast(Pair, w) >> 15;
+    return (__builtin_bit_cast(Pair, w & 0x7FFF7FFFu) ^ sign) - sign;
+}
+__device__ __forceinline__ uint16_t half_of_order(int order)
+{
+    return static_cast<uint16_t>(order < 0 ? 0x8000 | -order : order);
+}
 
 // The key of a value: its order, with the column's bits in the place of the lowest.
 __device__ __forceinline__ int key_of(float y, int cols, int column)
@@ -36,7 +47,14 @@ __device__ __forceinline__ int key_of(float y, int cols, int column)
     return __builtin_amdgcn_bitop3_b32(in_order(bits_of(y)), cols, column, 0xBA);       // (a & ~b) | c
 }
 
-constexpr int kNoKey = static_cast<int>(0x807FFFFF);     // keys up to this one stand for -inf
+// Keys up to kNoKey stand for -inf: the order of binary32 -inf, and of a 16-bit one in the upper half, with
+// any column below.
+template <class D, bool ROUNDED>
+constexpr int no_key()
+{
+    if constexpr (ROUNDED) return static_cast<int>(0x807FFFFFu);
+    else return static_cast<int>(((0x10000u - D::kInfBits) << 16) | 0xFFFFu);
+}
 
 __device__ __forceinline__ void order(int &a, int &b)     // the larger one first
 {
@@ -93,26 +111,38 @@ __device__ __forceinline__ void largest(int (&a)[S])
 struct Choice {
     int slot;                    // key of the lane's slot; kNoKey or less: there is none
     int top;                     // the largest key of the row, in all lanes
-    bool unsure;                 // keys do not tell the order
+    bool close;                  // keys do not tell the order of two slots
+    bool unsure;                 // keys do not tell the last slot
 };
 
+// Lanes that are number R of their group.
+template <int L>
+constexpr uint64_t lanes_at(int r)
+{
+    uint64_t m = 0;
+    for (int i = r; i < kWave; i += L) m |= 1ull << i;
+    return m;
+}
+
 // Slot R: the largest head of all lists in key[0 .. N-1] is taken, and its list moves up.
-template <int L, int V, int KL, int N, int R>
-__device__ __forceinline__ void take(int (&key)[V], int top_k, bool rounded, int l, int mine, int before,
-                                     Choice &c)
+template <int L, int V, int KL, int N, int R, bool ROUNDED, int NONE>
+__device__ __forceinline__ void take(int (&key)[V], int top_k, int mine, int before, Choice &c)
 {
     constexpr int kCols = L * V - 1;
-    if (R > top_k || (R == top_k && !rounded)) return;
+    if (R > top_k || (R == top_k && !ROUNDED)) return;
     const int head = key[0] | mine;
     const int best = group_max<L>(head);
     if constexpr (R == 0) c.top = best;
-    if constexpr (R > 0) c.unsure = c.unsure || (((best ^ before) & ~kCols) == 0 && best > kNoKey);
+    bool same = false;
+    if constexpr (ROUNDED && R > 0) same = ((best ^ before) & ~kCols) == 0 && best > NONE;
     if (R == top_k) {
+        c.unsure = same;
         if constexpr (N < V) c.unsure = c.unsure || key[0] == INT_MIN;   // a list that ends too early
         return;
     }
     if constexpr (R < KL) {
-        c.slot = l == R ? best : c.slot;
+        c.close = c.close || same;
+        c.slot = __builtin_amdgcn_inverse_ballot_w64(lanes_at<L>(R)) ? best : c.slot;
         const bool won = head == best;
         // (both values are read before one is picked: a pick between two places would make the list memory)
 #pragma unroll
@@ -121,23 +151,39 @@ __device__ __forceinline__ void take(int (&key)[V], int top_k, bool rounded, int
             if (i + R < KL) key[i] = won ? next : here;
         }
         if constexpr (N + R <= KL) key[N - 1] = won ? INT_MIN : key[N - 1];
-        take<L, V, KL, N, R + 1>(key, top_k, rounded, l, mine, best, c);
+        take<L, V, KL, N, R + 1, ROUNDED, NONE>(key, top_k, mine, best, c);
     }
 }
 
-// The top_k <= KL largest keys of every group, slot j's in lane j.  If `rounded`, keys have lost bits, and
-// one key more is looked at.  The keys are used up.
-template <int L, int V, int KL>
-__device__ __forceinline__ Choice choose(int (&key)[V], int top_k, bool rounded, int l)
+// The top_k <= KL largest keys of every group, slot j's in lane j.  The keys are used up.
+template <int L, int V, int KL, bool ROUNDED, int NONE>
+__device__ __forceinline__ Choice choose(int (&key)[V], int top_k, int l)
 {
     constexpr int N = V < KL ? V : KL;
     largest<N, 0, V>(key);
-    Choice c{kNoKey, kNoKey, false};
-    take<L, V, KL, N, 0>(key, top_k, rounded, l, ((L - 1) ^ l) * kRun, 0, c);   // (the lane's part of the columns)
+    Choice c{NONE, NONE, false, false};
+    take<L, V, KL, N, 0, ROUNDED, NONE>(key, top_k, ((L - 1) ^ l) * kRun, 0, c);    // (the lane's part of the column)
     return c;
 }
 
-// The same by values y (-inf: not to be chosen): column of slot l, or -1.
+// The right columns in the wrong order: every slot goes as many places down as slots are ahead of it by
+// whole values y and columns.
+template <int L>
+__device__ __forceinline__ int by_value(int index, float y, int top_k, int lane)
+{
+    const int first = lane & ~(L - 1), l = lane & (L - 1);
+    const int col = index >= 0 ? index : INT_MAX - kWave + l;
+    int rank = 0;
+    for (int r = 0; r < top_k; ++r) {
+        const float other = __shfl(y, first + r);
+        const int at = __shfl(col, first + r);
+        rank += other > y || (other == y && at < col) ? 1 : 0;
+    }
+    // (lanes beyond the slots keep to themselves)
+    return __builtin_amdgcn_ds_permute((first + (l < top_k ? rank : l)) * 4, index);
+}
+
+// The choice by whole values y (-inf: not to be chosen): column of slot l, or -1.
 template <int L, int V>
 __device__ __forceinline__ int choose_by_value(float (&y)[V], int top_k, int l)
 {
@@ -161,28 +207,47 @@ __device__ __forceinline__ int choose_by_value(float (&y)[V], int top_k, int l)
 
 // ---- rows ------------------------------------------------------------------------------------
 
-// y = x + bias, the keys as floats; without a bias -0 becomes +0, which equals it.
-template <int L, int V>
-__device__ __forceinline__ void add_bias(const RouteArgs &a, int l, const float (&x)[V], float (&y)[V])
+// A bias as it is added: NaN counts as -inf and +inf as the largest number, so that the sum with -inf stays
+// -inf; +0 for -0, so that zeros are alike.
+__device__ __forceinline__ float bias_of(float b)
 {
-    if (a.bias) {
-        const int at = anew(l * kRun);
+    return (b == b ? fminf(b, 3.402823466e38f) : -kInf) + 0.0f;
+}
+
+// y = x + bias, the order of the choice; without a bias -0 becomes +0, which equals it.
+template <int L, int V>
+__device__ __forceinline__ void add_bias(const RouteArgs &a, int l, int shape, const float (&x)[V], float (&y)[V])
+{
+    if (!a.bias) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            // NaN counts as -inf and +inf as the largest number: the sum with -inf stays -inf
-            float b = a.bias[min(column_of<L>(j) + at, a.experts - 1)];
-            b = b == b ? fminf(b, 3.402823466e38f) : -kInf;
-            y[j] = x[j] + (b + 0.0f);
+        for (int j = 0; j < V; ++j) y[j] = x[j] + 0.0f;
+        return;
+    }
+    const int at = anew(l * kRun);
+    if (shape != kSingle && a.bias_runs) {
+        float4 b[V / kRun];
+#pragma unroll
+        for (int q = 0; q < V / kRun; ++q) {
+            const int col = q * (L * kRun) + at;
+            b[q] = *reinterpret_cast<const float4 *>(a.bias + (col < a.experts ? col : 0));
+        }
+#pragma unroll
+        for (int q = 0; q < V / kRun; ++q) {
+            y[q * kRun] = x[q * kRun] + bias_of(b[q].x);
+            y[q * kRun + 1] = x[q * kRun + 1] + bias_of(b[q].y);
+            y[q * kRun + 2] = x[q * kRun + 2] + bias_of(b[q].z);
+            y[q * kRun + 3] = x[q * kRun + 3] + bias_of(b[q].w);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = x[j] + 0.0f;
+        for (int j = 0; j < V; ++j)
+            y[j] = x[j] + bias_of(a.bias[min(column_of<L>(j) + at, a.experts - 1)]);
     }
 }
 
 // A workgroup per chunk of rows, cut where a segment ends; probabilities are summed in registers,
 // slots counted in LDS, and the waves' sums added in order at the end of every part.
-template <class D, int L, int V, int KL, bool SUMS>
+template <class D, int L, int V, int KL, bool ROUNDED, bool SUMS>
 __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int shape)
 {
     constexpr int C = L * V, G = kWave / L, kCols = C - 1;
@@ -195,8 +260,11 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
     const int l = lane & (L - 1), g = lane / L;
     const bool sigmoid = (a.flags & NIMBLE_MOE_SIGMOID) != 0;
     const bool renorm = (a.flags & NIMBLE_MOE_RENORM) != 0;
-    const bool rounded = D::kWide || a.bias != nullptr;
-    const float nan = __builtin_nanf("");
+    constexpr int kNoKey = no_key<D, ROUNDED>();
+    // (made anew, so that the compiler does not fold it into what it is multiplied with)
+    const float nan = float_of(anew(0x7FC00000));
+    // scores of all experts are wanted for sums and for weights that are divided by their sum
+    const bool all_scores = SUMS || !(renorm || sigmoid);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
@@ -218,54 +286,83 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
             const bool live = inside && (!a.keep || a.keep[row] != 0);
             const auto *logits = static_cast<const typename D::Raw *>(a.logits) + row * a.stride;
-            float x[V];
-            load_row<D, L, V>(logits, a.experts, l, shape, x);
-            if (__ballot(live) != ~0ull) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[j] = live ? x[j] : -kInf;
-            }
-            Choice c;
+            const int top_k = anew_uniform(a.top_k);
+            RowOf<D, L, V> raw;
+            raw.load(logits, a.experts, l, shape);
+            if (__ballot(live) != ~0ull) raw.drop(live);
+            float x[V], logit, top = 0.0f;
             int index;
-            {
+            bool bad = false;                                   // in one lane of a group, or in all of them
+            if constexpr (ROUNDED) {
                 float y[V];
                 int key[V];
-                add_bias<L, V>(a, l, x, y);
+                raw.values(x);
+                add_bias<L, V>(a, l, shape, x, y);
                 const int cols = anew(kCols);
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     key[j] = key_of(y[j], cols, kCols ^ column_of<L>(j) ^ ((L - 1) * kRun));
-                c = choose<L, V, KL>(key, anew_uniform(a.top_k), rounded, anew(l));
+                const Choice c = choose<L, V, KL, true, kNoKey>(key, top_k, anew(l));
                 index = c.slot > kNoKey ? ~c.slot & kCols : -1;
-                if (rounded && __ballot(c.unsure) != 0) {
-                    add_bias<L, V>(a, l, x, y);
-                    index = choose_by_value<L, V>(y, a.top_k, l);
+                if (__ballot(c.unsure) != 0) {
+                    add_bias<L, V>(a, l, shape, x, y);
+                    index = choose_by_value<L, V>(y, top_k, l);
                 }
+                logit = index >= 0 ? D::up(logits[index]) : -kInf;
+                if (__ballot(c.close && !c.unsure) != 0) {
+                    // (in a wave that has chosen by value already, this changes nothing)
+                    const float b = index >= 0 && a.bias ? bias_of(a.bias[index]) : 0.0f;
+                    index = by_value<L>(index, logit + b, top_k, lane);
+                    logit = index >= 0 ? D::up(logits[index]) : -kInf;
+                }
+                if (all_scores) {
+                    top = x[0];
+#pragma unroll
+                    for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
+                    top = group_max<L>(top);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) bad = bad || !(x[j] < kInf);
+                }
+            } else {
+                int key[V];
+                Pair low{0, 0};
+#pragma unroll
+                for (int w = 0; w < V / 2; ++w) {
+                    const Pair u = pair_in_order(raw.word[w]);
+                    const uint32_t both = __builtin_bit_cast(uint32_t, u);
+                    key[2 * w] = static_cast<int>(both << 16 | (kCols ^ column_of<L>(2 * w) ^ ((L - 1) * kRun)));
+                    key[2 * w + 1] = static_cast<int>((both & 0xFFFF0000u) |
+                                                      (kCols ^ column_of<L>(2 * w + 1) ^ ((L - 1) * kRun)));
+                    low = __builtin_elementwise_min(low, u);
+                }
+                const Choice c = choose<L, V, KL, false, kNoKey>(key, top_k, anew(l));
+                index = c.slot > kNoKey ? ~c.slot & kCols : -1;
+                logit = index >= 0 ? D::up(half_of_order(c.slot >> 16)) : -kInf;
+                top = c.top > kNoKey ? D::up(half_of_order(c.top >> 16)) : -kInf;
+                if (all_scores) raw.values(x);
+                else bad = min(low.x, low.y) < -D::kInfBits || c.top >> 16 >= D::kInfBits;
             }
             const bool chosen = __shfl(index, lane & ~(L - 1)) >= 0;
-            float top, logit;
-            if (rounded) {
-                top = x[0];
-#pragma unroll
-                for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-                top = group_max<L>(top);
-                logit = index >= 0 ? D::up(logits[index]) : -kInf;
-            } else {
-                top = c.top > kNoKey ? float_of(in_order(c.top) & ~kCols) : -kInf;
-                logit = index >= 0 ? float_of(in_order(c.slot) & ~kCols) : -kInf;
-            }
             const Shifted by(shift_of(sigmoid, top));
-            scores_of<V>(sigmoid, x, by);
-            float sum = 0.0f;
+            float inv = 0.0f;
+            if (all_scores) {
+                scores_of<V>(sigmoid, x, by);
+                float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum = sum + x[j];
-            sum = group_sum<L>(sum);
-            const bool bad = !(sum == sum) || top == kInf;
-            const float inv = __builtin_amdgcn_rcpf(sum);
+                for (int j = 0; j < V; ++j) sum = sum + x[j];
+                sum = group_sum<L>(sum);
+                bad = !(sum == sum) || top == kInf;
+                inv = __builtin_amdgcn_rcpf(sum);
+            } else {
+                const unsigned long long group = (L == kWave ? ~0ull : (1ull << (L & 63)) - 1) << (lane & ~(L - 1));
+                bad = (__ballot(bad) & group) != 0;
+            }
             float w;
             if (renorm) {
                 const float t = group_max<16>(logit);
                 const float u = score_of(sigmoid, logit, Shifted(shift_of(sigmoid, t)));
-                w = u / group_sum<16>(u);
+                w = u * __builtin_amdgcn_rcpf(group_sum<16>(u));
             } else {
                 w = sigmoid ? sigmoid_of(logit) : by.exp(logit) * inv;
             }
@@ -313,18 +410,26 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
     }
 }
 
-template <class D, int L, int V, int KL>
+template <class D, int L, int V, int KL, bool ROUNDED>
 hipError_t run(const RouteArgs &a, hipStream_t stream)
 {
     const int shape = shape_of(a.logits, a.stride, a.experts, L * V, sizeof(typename D::Raw));
     const dim3 grid(a.rows.chunks), block(kRowWaves * kWave);
     if (a.counts) {
         const size_t lds = sizeof(float) * ((kRowWaves + 1) * L * V + kRowWaves);
-        k_route<D, L, V, KL, true><<<grid, block, lds, stream>>>(a, shape);
+        k_route<D, L, V, KL, ROUNDED, true><<<grid, block, lds, stream>>>(a, shape);
     } else {
-        k_route<D, L, V, KL, false><<<grid, block, 0, stream>>>(a, shape);
+        k_route<D, L, V, KL, ROUNDED, false><<<grid, block, 0, stream>>>(a, shape);
     }
     return hipGetLastError();
+}
+
+template <class D, int L, int V, int KL>
+hipError_t run(const RouteArgs &a, hipStream_t stream)
+{
+    if constexpr (!D::kWide)
+        if (!a.bias) return run<D, L, V, KL, false>(a, stream);
+    return run<D, L, V, KL, true>(a, stream);
 }
 
 template <class D, int L, int V>

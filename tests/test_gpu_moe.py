@@ -155,6 +155,53 @@ def test_every_top_k_with_ties(B, k, E):
     assert set(got) == {"index", "weight"}
 
 
+@pytest.mark.parametrize("E,k", [(30, 8), (64, 2), (64, 3), (256, 8), (300, 4), (1000, 8), (1024, 16), (2048, 8)])
+@pytest.mark.parametrize("sums", [False, True])
+def test_values_that_differ_in_their_last_bits(B, E, k, sums):
+    """Binary32 logits a few steps apart, among the chosen ones, at the last slot and in all columns, of
+    both signs; a few rows of them among ordinary rows, and next to each other in one lane's columns."""
+    import torch
+    rng = np.random.default_rng(E + k)
+    T = 60
+    x = rng.normal(size=(T, E)).astype(np.float32)
+    steps = lambda n, width: (np.float32(3.25) + rng.integers(0, width, n).astype(np.float32)   # noqa: E731
+                              * np.float32(2.0 ** -22)).astype(np.float32)
+    for t in range(0, T, 5):
+        x[t] = steps(E, 5) * (1 if t % 2 else -1)                       # every column
+        n = min(E, k + 3)
+        x[t + 1, rng.permutation(E)[:n]] = steps(n, 1000)               # the chosen and some beyond
+        n = min(E, max(k - 1, 1))
+        x[t + 2, rng.permutation(E)[:n]] = steps(n, 3)                  # the chosen but one
+        x[t + 3, :min(E, 2 * k)] = np.sort(steps(min(E, 2 * k), 1 << 20))   # neighbours
+    form = dict(renorm=False, sigmoid=True) if sums else {}
+    got = run(B, torch.as_tensor(x).to("cuda:0"), k, sums=sums, **form)
+    check(got, x, k, **form)
+    bias = (rng.integers(0, 4, E) * 2.0 ** -21).astype(np.float32)      # and sums of 16-bit logits with a bias
+    h = torch.as_tensor(x).to("cuda:0", torch.float16)
+    got = run(B, h, k, sums=sums, bias=bias, **form)
+    check(got, h.float().cpu().numpy(), k, bias=bias, **form)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("E,k", [(64, 8), (128, 8), (256, 5), (256, 16), (512, 8), (1024, 8), (2048, 16)])
+def test_all_the_chosen_in_neighbouring_columns(B, dtype, E, k):
+    """The largest logits in runs of neighbours, so that few lanes hold them, in every order."""
+    import torch
+    rng = np.random.default_rng(E * k)
+    T = 40
+    x = rng.normal(size=(T, E))
+    for t in range(T):
+        at = int(rng.integers(0, E - k)) if t % 3 else 4 * int(rng.integers(0, (E - k) // 4 + 1))
+        x[t, at:at + k] = rng.permutation(np.linspace(5, 9, k))
+        if t % 4 == 0:                                 # one lane's columns and no others
+            cols = np.arange(4)[None, :] + np.arange(0, E, max(64, E // 16))[:, None]
+            cols = cols.ravel()[:k + 2]
+            x[t, cols] = 10 + rng.permutation(len(cols))
+    d = torch.as_tensor(x).to("cuda:0", getattr(torch, dtype))
+    got = run(B, d, k)
+    check(got, d.float().cpu().numpy(), k, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("E", [5, 64, 200, 1024])
