@@ -13,8 +13,8 @@
  *
  * Rows are tokens.  Segments are runs of rows -- the tokens of a source GPU, a sequence, a
  * micro-batch -- given by ascending offsets d_seg_ptr [n_segments + 1]: segment s has rows
- * d_seg_ptr[s] .. d_seg_ptr[s+1]-1 (none is fine).  Rows in no segment are neither read nor
- * written.  Offsets below 0 or beyond the rows are taken as 0 and the number of rows; offsets
+ * d_seg_ptr[s] .. d_seg_ptr[s+1]-1 (none is fine).  Rows in no segment make no difference and are
+ * not written.  Offsets below 0 or beyond the rows are taken as 0 and the number of rows; offsets
  * that do not ascend give unspecified values (never an access out of range).  A NULL d_seg_ptr
  * stands for one segment of all rows and needs n_segments = 1.
  *

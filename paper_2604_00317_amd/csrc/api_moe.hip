@@ -14,6 +14,8 @@ namespace {
 
 namespace moe = nimble::moe;
 
+constexpr int32_t kChunks = 1 << 20, kChunksOfSums = 1 << 9, kChunksOfGradient = 1 << 9;
+
 nimble_status_t bad(const char *what) { return report(NIMBLE_ERR_INVALID, what); }
 nimble_status_t too_large(const char *what) { return report(NIMBLE_ERR_RANGE, what); }
 
@@ -79,7 +81,7 @@ int64_t nimble_moe_route_scratch_bytes(int32_t tokens, int32_t experts, int32_t 
     if (tokens < 0 || experts < 1 || experts > NIMBLE_MOE_MAX_EXPERTS || n_segments < 1 ||
         n_segments > NIMBLE_MOE_MAX_SEGMENTS)
         return -1;
-    const int32_t chunk = moe::route_chunk(tokens, experts, true);
+    const int32_t chunk = moe::route_chunk(tokens, experts, kChunksOfSums);
     return 2 * part_bytes(tokens, chunk, n_segments, experts) + part_bytes(tokens, chunk, n_segments, 1);
 }
 
@@ -101,7 +103,7 @@ nimble_status_t nimble_moe_route(int32_t tokens, int32_t experts, int32_t top_k,
     const bool sums = d_counts || d_routed || d_prob_sum;
     if (sums && !(d_counts && d_routed && d_prob_sum))
         return bad("counts, routed and prob_sum are wanted together or not at all");
-    const int32_t chunk = moe::route_chunk(tokens, experts, sums);
+    const int32_t chunk = moe::route_chunk(tokens, experts, sums ? kChunksOfSums : kChunks);
     moe::RouteArgs a{};
     a.rows = rows_of(tokens, chunk, n_segments, d_seg_ptr);
     if (sums) {
@@ -176,7 +178,7 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
         return bad("counts, routed and grad_loss are given together or not at all");
     if (!std::isfinite(alpha)) return bad("alpha must be finite");
     moe::BackwardArgs a{};
-    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, true), n_segments, d_seg_ptr);
+    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, kChunksOfGradient), n_segments, d_seg_ptr);
     a.experts = experts;
     a.top_k = top_k;
     a.flags = flags;
@@ -190,6 +192,7 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
     a.alpha = alpha;
     a.counts = d_counts;
     a.routed = d_routed;
+    a.count_runs = reinterpret_cast<uintptr_t>(d_counts) % 16 == 0 && experts % 4 == 0;
     a.grad_loss = d_grad_loss;
     a.grad = d_grad_logits;
     a.grad_stride = grad_stride;

@@ -290,9 +290,8 @@ bool many_parts(const Rows &r) { return r.chunks > 8 * static_cast<int64_t>(r.se
 
 // Whole passes of a workgroup's rows; with sums no more than 512 chunks, two workgroups per CU, all
 // of them at work at once.
-int32_t route_chunk(int32_t tokens, int32_t experts, bool sums)
+int32_t route_chunk(int32_t tokens, int32_t experts, int32_t most)
 {
-    const int32_t most = sums ? 1 << 9 : 1 << 20;
     return round_up((static_cast<int64_t>(tokens) + most - 1) / most,
                     kRowWaves * (experts <= 256 ? 4 : experts <= 512 ? 2 : 1));
 }

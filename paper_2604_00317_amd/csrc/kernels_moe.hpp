@@ -50,6 +50,7 @@ struct BackwardArgs {
     const float *weight, *grad_weight;
     float alpha;
     const int32_t *counts, *routed;
+    bool count_runs;             // counts are made of runs of four, aligned to their size
     const float *grad_loss;
     void *grad;
     int64_t grad_stride;
@@ -63,7 +64,7 @@ struct CountArgs {
     int32_t *part;               // [chunks + segments][experts if counts][ranks if rank_tokens]
 };
 
-int32_t route_chunk(int32_t tokens, int32_t experts, bool sums);
+int32_t route_chunk(int32_t tokens, int32_t experts, int32_t most);
 int32_t count_chunk(int32_t tokens, int32_t top_k);
 
 hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream);

@@ -30,46 +30,66 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
     float *mine = slots[wave * G + g];
 #pragma unroll
     for (int j = 0; j < V; ++j) mine[column_of<L>(j) + l * kRun] = 0.0f;
+    // Rows are read a pass ahead; the first ones before it is known which segment they are in.
+    const auto *const logits = static_cast<const typename D::Raw *>(a.logits);
+    RowOf<D, L, V> ahead;
+    int ahead_of = lo + wave * G;
+    ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, hi - 1)) * a.stride, a.experts, l, shape);
     Segments segments(a.rows, lane);
     for (int s = segments.first(lo); s < a.rows.segments; ++s) {
         const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
         if (begin >= hi) break;
         if (from >= to) continue;
         float coef[V];
-        double unit = 0.0;
-        if (a.counts) {
-            const double n = static_cast<double>(a.routed[s]);
-            if (a.routed[s] != 0)
-                unit = static_cast<double>(a.grad_loss[s]) * static_cast<double>(a.alpha) * a.experts /
-                       (static_cast<double>(a.top_k) * n * n);
-        }
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int col = column_of<L>(j) + l * kRun;
-            coef[j] = a.counts && col < a.experts
-                          ? static_cast<float>(unit * a.counts[static_cast<int64_t>(s) * a.experts + col])
-                          : 0.0f;
+        for (int j = 0; j < V; ++j) coef[j] = 0.0f;
+        if (a.counts) {
+            const int32_t *counts = a.counts + static_cast<int64_t>(s) * a.experts;
+            const int at = anew(l * kRun);
+            int count[V];
+            if (shape != kSingle && a.count_runs) {
+#pragma unroll
+                for (int q = 0; q < V / kRun; ++q) {
+                    const int col = q * (L * kRun) + at;
+                    const int4 c = *reinterpret_cast<const int4 *>(counts + (col < a.experts ? col : 0));
+                    count[q * kRun] = c.x;
+                    count[q * kRun + 1] = c.y;
+                    count[q * kRun + 2] = c.z;
+                    count[q * kRun + 3] = c.w;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) count[j] = counts[min(column_of<L>(j) + at, a.experts - 1)];
+            }
+            const double n = static_cast<double>(a.routed[s]);
+            const double unit = static_cast<double>(a.grad_loss[s]) * static_cast<double>(a.alpha) * a.experts /
+                                (static_cast<double>(a.top_k) * n * n);
+            const float per_count = n != 0.0 ? static_cast<float>(unit) : 0.0f;
+            // (columns beyond the row's end have probability 0)
+#pragma unroll
+            for (int j = 0; j < V; ++j) coef[j] = per_count * static_cast<float>(count[j]);
         }
         for (int r0 = from + wave * G; r0 < to; r0 += kRowWaves * G) {
             const bool inside = r0 + g < to;
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
-            const bool kept = !a.keep || a.keep[row] != 0;
-            RowOf<D, L, V> raw;
-            raw.load(static_cast<const typename D::Raw *>(a.logits) + row * a.stride, a.experts, l, shape);
-            int index = -1;
-            float w = 0.0f, wg = 0.0f, gw = 0.0f;
-            bool nan = false;
-            if (kept && l < a.top_k) {
-                index = a.index[row * a.top_k + l];
-                if (static_cast<uint32_t>(index) >= static_cast<uint32_t>(a.experts)) index = -1;
-                w = a.weight[row * a.top_k + l];
-                nan = l == 0 && !(w == w);
-                if (index >= 0 && a.grad_weight) gw = a.grad_weight[row * a.top_k + l];
-                w = index >= 0 ? w : 0.0f;
-                wg = w * gw;
+            if (r0 != ahead_of)
+                ahead.load(logits + row * a.stride, a.experts, l, shape);
+            const RowOf<D, L, V> raw = ahead;
+            const int64_t slot = row * a.top_k + min(l, a.top_k - 1);   // (lanes without a slot read the last)
+            int index = a.index[slot];
+            float w = a.weight[slot], gw = a.grad_weight ? a.grad_weight[slot] : 0.0f;
+            if (r0 + kRowWaves * G < to) {
+                ahead_of = r0 + kRowWaves * G;
+                ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, to - 1)) * a.stride, a.experts, l, shape);
             }
+            const bool kept = !a.keep || a.keep[row] != 0;
+            const bool nan = kept && l == 0 && !(w == w);
+            const bool there = kept && l < a.top_k && static_cast<uint32_t>(index) < static_cast<uint32_t>(a.experts);
+            index = there ? index : -1;
+            w = there ? w : 0.0f;
+            const float wg = there ? w * gw : 0.0f;
             const float all = group_sum<16>(wg);
-            const float slope = w * (gw - (renorm ? all * per_scale : 0.0f));
+            const float slope = w * ((there ? gw : 0.0f) - (renorm ? all * per_scale : 0.0f));
             if (index >= 0 && inside) atomicAdd(&mine[index], slope);
             float x[V], sum = 0.0f, rest = 0.0f, r[V];
             raw.values(x);

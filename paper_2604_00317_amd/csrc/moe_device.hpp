@@ -13,6 +13,9 @@ namespace {
 constexpr float kInf = __builtin_inff();
 constexpr int kRowWaves = 8;         // waves of a workgroup that works on rows
 
+// Waves a SIMD should hold: two workgroups to a CU, where 128 registers do.
+constexpr int waves_per_simd(int values) { return values <= 16 ? 4 : 2; }
+
 // ---- element types ---------------------------------------------------------------------------
 
 struct F32 {

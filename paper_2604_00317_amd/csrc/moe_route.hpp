@@ -248,7 +248,7 @@ __device__ __forceinline__ void add_bias(const RouteArgs &a, int l, int shape, c
 // A workgroup per chunk of rows, cut where a segment ends; probabilities are summed in registers,
 // slots counted in LDS, and the waves' sums added in order at the end of every part.
 template <class D, int L, int V, int KL, bool ROUNDED, bool SUMS>
-__global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int shape)
+__global__ __launch_bounds__(kRowWaves *kWave, waves_per_simd(V)) void k_route(RouteArgs a, int shape)
 {
     constexpr int C = L * V, G = kWave / L, kCols = C - 1;
     extern __shared__ float lds[];
@@ -268,6 +268,11 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
+    // Rows are read a pass ahead; the first ones before it is known which segment they are in.
+    const auto *const logits = static_cast<const typename D::Raw *>(a.logits);
+    RowOf<D, L, V> ahead;
+    int ahead_of = lo + wave * G;
+    ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, hi - 1)) * a.stride, a.experts, l, shape);
     Segments segments(a.rows, lane);
     for (int s = segments.first(lo); s < a.rows.segments; ++s) {
         const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
@@ -284,11 +289,15 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
         for (int r0 = from + wave * G; r0 < to; r0 += kRowWaves * G) {
             const bool inside = r0 + g < to;
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
-            const bool live = inside && (!a.keep || a.keep[row] != 0);
-            const auto *logits = static_cast<const typename D::Raw *>(a.logits) + row * a.stride;
+            const auto *const mine = logits + row * a.stride;
             const int top_k = anew_uniform(a.top_k);
-            RowOf<D, L, V> raw;
-            raw.load(logits, a.experts, l, shape);
+            if (r0 != ahead_of) ahead.load(mine, a.experts, l, shape);
+            RowOf<D, L, V> raw = ahead;
+            if (r0 + kRowWaves * G < to) {
+                ahead_of = r0 + kRowWaves * G;
+                ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, to - 1)) * a.stride, a.experts, l, shape);
+            }
+            const bool live = inside && (!a.keep || a.keep[row] != 0);
             if (__ballot(live) != ~0ull) raw.drop(live);
             float x[V], logit, top = 0.0f;
             int index;
@@ -308,12 +317,12 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route(RouteArgs a, int sha
                     add_bias<L, V>(a, l, shape, x, y);
                     index = choose_by_value<L, V>(y, top_k, l);
                 }
-                logit = index >= 0 ? D::up(logits[index]) : -kInf;
+                logit = index >= 0 ? D::up(mine[index]) : -kInf;
                 if (__ballot(c.close && !c.unsure) != 0) {
                     // (in a wave that has chosen by value already, this changes nothing)
                     const float b = index >= 0 && a.bias ? bias_of(a.bias[index]) : 0.0f;
                     index = by_value<L>(index, logit + b, top_k, lane);
-                    logit = index >= 0 ? D::up(logits[index]) : -kInf;
+                    logit = index >= 0 ? D::up(mine[index]) : -kInf;
                 }
                 if (all_scores) {
                     top = x[0];
