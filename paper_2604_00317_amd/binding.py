@@ -50,6 +50,8 @@ EXPORTS = [
 ]
 
 _lib = None
+_torch = None               # the module, once the library is loaded
+_MOE_KINDS = {}             # element types of logits
 
 
 class NimbleError(RuntimeError):
@@ -60,7 +62,7 @@ class NimbleError(RuntimeError):
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     """Loads the in-tree library; builds it first only when no built library exists."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -72,7 +74,10 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     # HIP runtime.  torch brings its own copy: it is imported first, and the library's dependency
     # on the runtime then resolves to the copy already in the process (loaded the other way
     # round, torch finds a runtime it was not built for and reports no GPU).
-    import torch  # noqa: F401
+    import torch
+    _torch = torch
+    _MOE_KINDS.update({torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16,
+                       torch.bfloat16: NIMBLE_BF16})
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, i64, u32, dbl = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
                               ctypes.c_double)
@@ -383,8 +388,7 @@ def nimble_plan_quantize(topo: Topo, d_traffic, d_splits, iters: int, chi: int,
 # at once per call, and torch is asked for the bare stream.
 
 def _moe_wrong(t, dtype, numel, gpu, what):
-    import torch
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{what} must be a device tensor")
     if t.get_device() != gpu:
         raise ValueError(f"{what} must be on cuda:{gpu}, like the first tensor of the call")
@@ -392,9 +396,7 @@ def _moe_wrong(t, dtype, numel, gpu, what):
 
 
 def _moe_ptr(t, dtype, numel, gpu, what):
-    """Pointer of a contiguous tensor on that GPU; None stays None."""
-    if t is None:
-        return None
+    """Pointer of a contiguous tensor on that GPU."""
     try:
         if (t.dtype is dtype and t.numel() == numel and t.get_device() == gpu
                 and t.is_contiguous()):
@@ -408,17 +410,30 @@ def _moe_rows(t, dtype, rows, cols, gpu, what):
     """Pointer and row stride of a matrix whose rows are contiguous and do not overlap."""
     if t.dtype is not dtype or t.get_device() != gpu or t.shape != (rows, cols):
         _moe_wrong(t, dtype, rows * cols, gpu, what)
-    if rows < 2 or t.is_contiguous():
-        if rows == 1 and cols > 1 and t.stride(1) != 1:
-            raise ValueError(f"rows of {what} must be contiguous")
+    if t.is_contiguous():
         return t.data_ptr(), cols
-    if (cols > 1 and t.stride(1) != 1) or t.stride(0) < cols:
+    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
         raise ValueError(f"rows of {what} must be contiguous and must not overlap")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _moe_logits(t, d_index):
+    """(GPU, element type, tokens, experts, top_k, pointer, row stride) of a call on logits, all
+    other tensors of which have to be on the same GPU."""
+    kind = _MOE_KINDS.get(t.dtype)
+    if kind is None:
+        raise ValueError("d_logits must be float32, float16 or bfloat16")
+    gpu = _moe_gpu(t, "d_logits")
+    if t.dim() != 2:
+        raise ValueError("d_logits must be [tokens][experts]")
+    tokens, experts = t.shape
+    if d_index.dim() != 2 or d_index.size(0) != tokens:
+        raise ValueError("d_index must be [tokens][top_k]")
+    x, stride = _moe_rows(t, t.dtype, tokens, experts, gpu, "d_logits")
+    return gpu, kind, tokens, experts, d_index.size(1), x, stride
 
 
 def _moe_gpu(t, what):
-    """Index of the GPU the first tensor of a call is on; all others have to be there."""
     try:
         gpu = t.get_device()
     except AttributeError:
@@ -429,9 +444,8 @@ def _moe_gpu(t, what):
 
 
 def _moe_stream(stream, gpu):
-    import torch
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(gpu)
+        return _torch._C._cuda_getCurrentRawStream(gpu)
     if stream.device.index != gpu:
         raise ValueError("the stream is on another GPU than the tensors")
     return stream.cuda_stream
@@ -440,15 +454,15 @@ def _moe_stream(stream, gpu):
 def _moe_scratch(t, nbytes, gpu, stream):
     """(pointer, bytes, owner) of scratch memory: the tensor given, or memory of the call's own
     stream, which torch hands out again only behind the call's work."""
-    import torch
     if nbytes < 0:
         return None, 0, None                 # sizes the library refuses: it says why
     if t is None:
+        where = _torch.device("cuda", gpu)
         if stream is None:
-            t = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", gpu))
+            t = _torch.empty(nbytes, dtype=_torch.uint8, device=where)
         else:
-            with torch.cuda.stream(stream):
-                t = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", gpu))
+            with _torch.cuda.stream(stream):
+                t = _torch.empty(nbytes, dtype=_torch.uint8, device=where)
         return t.data_ptr(), nbytes, t
     if t.get_device() != gpu or not t.is_contiguous():
         raise ValueError(f"d_scratch must be contiguous and on cuda:{gpu}")
@@ -456,39 +470,13 @@ def _moe_scratch(t, nbytes, gpu, stream):
 
 
 def _moe_run(gpu, fn, *args):
-    import torch
-    if torch._C._cuda_getDevice() == gpu:
+    if _torch._C._cuda_getDevice() == gpu:
         status = fn(*args)
     else:
-        with torch.cuda.device(gpu):
+        with _torch.cuda.device(gpu):
             status = fn(*args)
-    if status != NIMBLE_OK:
+    if status:
         raise NimbleError(status, nimble_last_error())
-
-
-def _moe_dtype(t):
-    import torch
-    kind = {torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16,
-            torch.bfloat16: NIMBLE_BF16}.get(t.dtype)
-    if kind is None:
-        raise ValueError("d_logits must be float32, float16 or bfloat16")
-    if t.dim() != 2:
-        raise ValueError("d_logits must be [tokens][experts]")
-    return kind
-
-
-def _moe_top_k(d_index, tokens):
-    if d_index.dim() != 2 or d_index.size(0) != tokens:
-        raise ValueError("d_index must be [tokens][top_k]")
-    return d_index.size(1)
-
-
-def _moe_flags(sigmoid: bool, renorm: bool) -> int:
-    return (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0)
-
-
-def _moe_segments(d_seg_ptr) -> int:
-    return 1 if d_seg_ptr is None else d_seg_ptr.numel() - 1
 
 
 def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, renorm: bool = True,
@@ -497,29 +485,32 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
     """Chooses d_index.shape[1] experts per row of d_logits [tokens][experts] (float32, float16 or
     bfloat16; rows may be strided), with their weights.  d_counts [segments][experts], d_routed
     [segments] and d_prob_sum [segments][experts] are wanted together or not at all."""
-    import torch
-    i32, f32 = torch.int32, torch.float32
-    lib = load_library()
-    kind = _moe_dtype(d_logits)
-    gpu = _moe_gpu(d_logits, "d_logits")
-    tokens, experts = d_logits.shape
-    top_k = _moe_top_k(d_index, tokens)
-    n_seg = _moe_segments(d_seg_ptr)
-    x, stride = _moe_rows(d_logits, d_logits.dtype, tokens, experts, gpu, "d_logits")
-    scratch = nbytes = owner = None
+    lib = _lib or load_library()
+    i32, f32 = _torch.int32, _torch.float32
+    gpu, kind, tokens, experts, top_k, x, stride = _moe_logits(d_logits, d_index)
+    bias = keep = seg = counts = routed = prob = scratch = owner = None
+    n_seg, nbytes = 1, 0
+    if d_seg_ptr is not None:
+        n_seg = d_seg_ptr.numel() - 1
+        seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
+    if d_bias is not None:
+        bias = _moe_ptr(d_bias, f32, experts, gpu, "d_bias")
+    if d_keep is not None:
+        keep = _moe_ptr(d_keep, _torch.uint8, tokens, gpu, "d_keep")
     if d_counts is not None:
+        counts = _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts")
         scratch, nbytes, owner = _moe_scratch(
             d_scratch, lib.nimble_moe_route_scratch_bytes(tokens, experts, n_seg), gpu, stream)
-    _moe_run(gpu, lib.nimble_moe_route, tokens, experts, top_k, _moe_flags(sigmoid, renorm), kind, x,
-             stride, _moe_ptr(d_bias, f32, experts, gpu, "d_bias"),
-             _moe_ptr(d_keep, torch.uint8, tokens, gpu, "d_keep"), scale, n_seg,
-             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
+    if d_routed is not None:
+        routed = _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed")
+    if d_prob_sum is not None:
+        prob = _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum")
+    _moe_run(gpu, lib.nimble_moe_route, tokens, experts, top_k,
+             (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
+             stride, bias, keep, scale, n_seg, seg,
              _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
-             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"),
-             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
-             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
-             _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum"), scratch, nbytes or 0,
-             _moe_stream(stream, gpu))
+             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), counts, routed, prob, scratch,
+             nbytes, _moe_stream(stream, gpu))
 
 
 def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 1) -> int:
@@ -529,16 +520,17 @@ def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 
 def nimble_moe_balance_loss(d_counts, d_routed, d_prob_sum, top_k: int, alpha: float, d_loss,
                             stream=None) -> None:
     """d_loss [segments] from the sums nimble_moe_route gives."""
-    import torch
+    lib = _lib or load_library()
+    i32, f32 = _torch.int32, _torch.float32
     gpu = _moe_gpu(d_counts, "d_counts")
     if d_counts.dim() != 2:
         raise ValueError("d_counts must be [segments][experts]")
     n_seg, experts = d_counts.shape
-    _moe_run(gpu, load_library().nimble_moe_balance_loss, n_seg, experts, top_k,
-             _moe_ptr(d_counts, torch.int32, n_seg * experts, gpu, "d_counts"),
-             _moe_ptr(d_routed, torch.int32, n_seg, gpu, "d_routed"),
-             _moe_ptr(d_prob_sum, torch.float32, n_seg * experts, gpu, "d_prob_sum"), alpha,
-             _moe_ptr(d_loss, torch.float32, n_seg, gpu, "d_loss"), _moe_stream(stream, gpu))
+    _moe_run(gpu, lib.nimble_moe_balance_loss, n_seg, experts, top_k,
+             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
+             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
+             _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum"), alpha,
+             _moe_ptr(d_loss, f32, n_seg, gpu, "d_loss"), _moe_stream(stream, gpu))
 
 
 def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sigmoid: bool = False,
@@ -547,51 +539,62 @@ def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sig
                               d_grad_loss=None, stream=None) -> None:
     """Gradient of the logits from those of weights and loss, with the flags, scale, d_keep and
     segments of the call of nimble_moe_route that gave d_index and d_weight."""
-    import torch
-    i32, f32 = torch.int32, torch.float32
-    kind = _moe_dtype(d_logits)
-    gpu = _moe_gpu(d_logits, "d_logits")
-    tokens, experts = d_logits.shape
-    top_k = _moe_top_k(d_index, tokens)
-    n_seg = _moe_segments(d_seg_ptr)
-    x, stride = _moe_rows(d_logits, d_logits.dtype, tokens, experts, gpu, "d_logits")
+    lib = _lib or load_library()
+    i32, f32 = _torch.int32, _torch.float32
+    gpu, kind, tokens, experts, top_k, x, stride = _moe_logits(d_logits, d_index)
     dx, grad_stride = _moe_rows(d_grad_logits, d_logits.dtype, tokens, experts, gpu,
                                 "d_grad_logits")
-    _moe_run(gpu, load_library().nimble_moe_route_backward, tokens, experts, top_k,
-             _moe_flags(sigmoid, renorm), kind, x, stride,
-             _moe_ptr(d_keep, torch.uint8, tokens, gpu, "d_keep"), scale, n_seg,
-             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
+    keep = seg = grad_weight = counts = routed = grad_loss = None
+    n_seg = 1
+    if d_seg_ptr is not None:
+        n_seg = d_seg_ptr.numel() - 1
+        seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
+    if d_keep is not None:
+        keep = _moe_ptr(d_keep, _torch.uint8, tokens, gpu, "d_keep")
+    if d_grad_weight is not None:
+        grad_weight = _moe_ptr(d_grad_weight, f32, tokens * top_k, gpu, "d_grad_weight")
+    if d_counts is not None:
+        counts = _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts")
+    if d_routed is not None:
+        routed = _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed")
+    if d_grad_loss is not None:
+        grad_loss = _moe_ptr(d_grad_loss, f32, n_seg, gpu, "d_grad_loss")
+    _moe_run(gpu, lib.nimble_moe_route_backward, tokens, experts, top_k,
+             (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
+             stride, keep, scale, n_seg, seg,
              _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
-             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"),
-             _moe_ptr(d_grad_weight, f32, tokens * top_k, gpu, "d_grad_weight"), alpha,
-             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
-             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
-             _moe_ptr(d_grad_loss, f32, n_seg, gpu, "d_grad_loss"), dx, grad_stride,
-             _moe_stream(stream, gpu))
+             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), grad_weight, alpha, counts,
+             routed, grad_loss, dx, grad_stride, _moe_stream(stream, gpu))
 
 
 def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=None,
                       d_rank_tokens=None, d_seg_ptr=None, d_scratch=None, stream=None) -> None:
     """Slots per expert (d_counts [segments][experts]) and distinct tokens per destination GPU
     (d_rank_tokens [segments][ranks], by d_expert_rank [experts]) of routed tokens."""
-    import torch
-    i32 = torch.int32
-    lib = load_library()
+    lib = _lib or load_library()
+    i32 = _torch.int32
     gpu = _moe_gpu(d_index, "d_index")
-    tokens = d_index.size(0)
-    top_k = _moe_top_k(d_index, tokens)
-    n_seg = _moe_segments(d_seg_ptr)
-    ranks = 0 if d_rank_tokens is None else d_rank_tokens.size(-1)
+    if d_index.dim() != 2:
+        raise ValueError("d_index must be [tokens][top_k]")
+    tokens, top_k = d_index.shape
+    seg = place = counts = rank_tokens = None
+    n_seg, ranks = 1, 0
+    if d_seg_ptr is not None:
+        n_seg = d_seg_ptr.numel() - 1
+        seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
+    if d_expert_rank is not None:
+        place = _moe_ptr(d_expert_rank, i32, experts, gpu, "d_expert_rank")
+    if d_counts is not None:
+        counts = _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts")
+    if d_rank_tokens is not None:
+        ranks = d_rank_tokens.size(-1)
+        rank_tokens = _moe_ptr(d_rank_tokens, i32, n_seg * ranks, gpu, "d_rank_tokens")
     scratch, nbytes, owner = _moe_scratch(
         d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg), gpu,
         stream)
     _moe_run(gpu, lib.nimble_moe_counts, tokens, top_k,
-             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"), experts, n_seg,
-             _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr"),
-             _moe_ptr(d_expert_rank, i32, experts, gpu, "d_expert_rank"), ranks,
-             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
-             _moe_ptr(d_rank_tokens, i32, n_seg * ranks, gpu, "d_rank_tokens"), scratch, nbytes,
-             _moe_stream(stream, gpu))
+             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"), experts, n_seg, seg, place,
+             ranks, counts, rank_tokens, scratch, nbytes, _moe_stream(stream, gpu))
 
 
 def nimble_moe_counts_scratch_bytes(tokens: int, top_k: int, experts: int, n_ranks: int = 0,
@@ -604,18 +607,22 @@ def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traf
                        d_dst=None, way_back: bool = False, stream=None) -> None:
     """Demand vectors d_traffic [batch][n_comm] of d_rank_tokens, [batch][ranks][ranks] or the
     [batch * ranks][ranks] that nimble_moe_counts fills with a segment per source GPU."""
-    import torch
-    i32 = torch.int32
+    lib = _lib or load_library()
+    i32 = _torch.int32
     gpu = _moe_gpu(d_rank_tokens, "d_rank_tokens")
     ranks = d_rank_tokens.size(-1)
     if batch < 1 or d_traffic.numel() % batch:
         raise ValueError("d_traffic must be [batch][commodities]")
     n_comm = d_traffic.numel() // batch
-    _moe_run(gpu, load_library().nimble_moe_traffic, batch, ranks,
+    src = dst = None
+    if d_src is not None:
+        src = _moe_ptr(d_src, i32, n_comm, gpu, "d_src")
+    if d_dst is not None:
+        dst = _moe_ptr(d_dst, i32, n_comm, gpu, "d_dst")
+    _moe_run(gpu, lib.nimble_moe_traffic, batch, ranks,
              _moe_ptr(d_rank_tokens, i32, batch * ranks * ranks, gpu, "d_rank_tokens"),
-             bytes_per_token, n_comm, _moe_ptr(d_src, i32, n_comm, gpu, "d_src"),
-             _moe_ptr(d_dst, i32, n_comm, gpu, "d_dst"), NIMBLE_MOE_WAY_BACK if way_back else 0,
-             _moe_ptr(d_traffic, torch.float64, batch * n_comm, gpu, "d_traffic"),
+             bytes_per_token, n_comm, src, dst, NIMBLE_MOE_WAY_BACK if way_back else 0,
+             _moe_ptr(d_traffic, _torch.float64, batch * n_comm, gpu, "d_traffic"),
              _moe_stream(stream, gpu))
 
 

@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <climits>
+
 #include "../../include/nimble_moe.h"
 #include "kernels_moe.hpp"
 #include "wave_ops.hpp"
@@ -91,6 +93,14 @@ __device__ __forceinline__ int group_max(int v)
         v = max(h.a, h.b);
     }
     return v;
+}
+// Over the wave, as a scalar: rows pass theirs on to the last one, half the instructions of an exchange.
+__device__ __forceinline__ int wave_max(int v)
+{
+    v = group_max<16>(v);
+    v = max(v, __builtin_amdgcn_update_dpp(INT_MIN, v, 0x142, 0xA, 0xF, false));   // row_bcast:15
+    v = max(v, __builtin_amdgcn_update_dpp(INT_MIN, v, 0x143, 0xC, 0xF, false));   // row_bcast:31
+    return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 template <int L>
 __device__ __forceinline__ float group_max(float v)

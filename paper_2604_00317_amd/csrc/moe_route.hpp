@@ -131,7 +131,9 @@ __device__ __forceinline__ void take(int (&key)[V], int top_k, int mine, int bef
     constexpr int kCols = L * V - 1;
     if (R > top_k || (R == top_k && !ROUNDED)) return;
     const int head = key[0] | mine;
-    const int best = group_max<L>(head);
+    int best;
+    if constexpr (L == kWave) best = wave_max(head);
+    else best = group_max<L>(head);
     if constexpr (R == 0) c.top = best;
     bool same = false;
     if constexpr (ROUNDED && R > 0) same = ((best ^ before) & ~kCols) == 0 && best > NONE;
@@ -325,10 +327,14 @@ __global__ __launch_bounds__(kRowWaves *kWave, waves_per_simd(V)) void k_route(R
                     logit = index >= 0 ? D::up(mine[index]) : -kInf;
                 }
                 if (all_scores) {
-                    top = x[0];
+                    // any shift near the largest logit does, so without a bias the largest key gives one
+                    top = c.top > kNoKey ? float_of(in_order(c.top)) : -kInf;
+                    if (a.bias || __ballot(top == -kInf || fabsf(top) <= 512.0f) != ~0ull) {
+                        top = x[0];
 #pragma unroll
-                    for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-                    top = group_max<L>(top);
+                        for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
+                        top = group_max<L>(top);
+                    }
                 } else {
 #pragma unroll
                     for (int j = 0; j < V; ++j) bad = bad || !(x[j] < kInf);
