@@ -110,11 +110,12 @@ __global__ __launch_bounds__(256) void k_balance_loss(int experts, double unit, 
 
 // ---- counts and demand -----------------------------------------------------------------------
 
-// Counts.  A thread has whole rows; what bounds the kernel is LDS additions to few places: most rows of
-// a skewed router choose the same experts.  So every bin is there `copies` times, side by side in
-// different banks, one for every copies-th lane.  GPUs are not counted slot by slot: their tokens are the
-// slots of their experts, added up at the end, less the slots that go where an earlier slot of the
-// same row goes, which are few.
+// Counts.  A thread has whole rows.  What bounds the kernel, behind the reading of the indices, is LDS
+// additions to few places -- most rows of a skewed router choose the same experts -- and the
+// comparisons of a row's destinations.  So every bin is there several times, side by side in different
+// banks, a copy for every so many'th lane; indices of no expert have a bin of their own instead of a branch.
+// GPUs are not counted slot by slot: their tokens are the slots of their experts, added up at the
+// end, less the slots that go where an earlier slot of the same row goes, which are few.
 constexpr int kCountBlock = 512;
 
 // Rows a thread reads before it counts them.
@@ -122,37 +123,41 @@ template <int K>
 constexpr int rows_at_once() { return K <= 4 ? 4 : K <= 8 ? 2 : 1; }
 
 template <int K>
-__global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies, int dup_copies, bool aligned)
+__global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_copies, int log_dups, bool aligned)
 {
     constexpr int N = rows_at_once<K>();
     extern __shared__ int lds[];
     const int E = a.experts, R = a.rank_tokens ? a.ranks : 0;
-    int *bins = lds;                                 // [experts][copies]
-    int *dups = bins + E * copies;                   // [ranks][dup_copies]
-    int *totals = dups + R * dup_copies;             // [ranks]
-    int *place = totals + R;                         // [experts]
+    int *bins = lds;                                 // [experts + 1][copies]
+    int *dups = bins + ((E + 1) << log_copies);      // [ranks][copies of theirs]
+    int *totals = dups + (R << log_dups);            // [ranks]
+    int *place = totals + R;                         // [experts + 1]; below 0, each its own: nowhere
     const int lane = threadIdx.x & (kWave - 1);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
+    const int copies = 1 << log_copies, dup_copies = 1 << log_dups;
     const int copy = threadIdx.x & (copies - 1), dup_copy = threadIdx.x & (dup_copies - 1);
-    if (R)
-        for (int e = threadIdx.x; e < E; e += kCountBlock) place[e] = a.place[e];
+    if (R) {
+        for (int e = threadIdx.x; e <= E; e += kCountBlock) {
+            const int r = e < E ? a.place[e] : -1;
+            place[e] = static_cast<uint32_t>(r) < static_cast<uint32_t>(R) ? r : -1 - e;
+        }
+    }
     Segments segments(a.rows, lane);
     for (int s = segments.first(lo); s < a.rows.segments; ++s) {
         const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
         if (begin >= hi) break;
         if (from >= to) continue;
-        for (int c = threadIdx.x; c < E * copies + R * (dup_copies + 1); c += kCountBlock) lds[c] = 0;
+        for (int c = threadIdx.x; c < ((E + 1) << log_copies) + (R << log_dups) + R; c += kCountBlock) lds[c] = 0;
         __syncthreads();
         for (int64_t u0 = from; u0 < to; u0 += N * kCountBlock) {
-            const int64_t r0 = u0 + threadIdx.x;
             int idx[N][K];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 if (u0 + n * kCountBlock >= to) break;
-                // (a row that is not there is read as the part's last one, and its indices dropped)
-                const int64_t row = r0 + n * kCountBlock;
+                // (a row that is not there is read as the part's last one, and counts as no expert)
+                const int64_t row = u0 + n * kCountBlock + threadIdx.x;
                 const int32_t *p = a.index + min(row, static_cast<int64_t>(to) - 1) * K;
                 if (K % 4 == 0 && aligned) {
 #pragma unroll
@@ -178,24 +183,25 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies,
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 if (u0 + n * kCountBlock >= to) break;
-                const bool inside = r0 + n * kCountBlock < to;
-                int to_rank[K];
+                if (u0 + (n + 1) * kCountBlock > to) {                // the last rows of the part
+                    const bool inside = u0 + n * kCountBlock + threadIdx.x < to;
+#pragma unroll
+                    for (int j = 0; j < K; ++j) idx[n][j] = inside ? idx[n][j] : -1;
+                }
+                int rank[K];
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
-                    const int e = idx[n][j];
-                    const bool there = inside && static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
-                    if (there) atomicAdd(&bins[e * copies + copy], 1);
-                    if (R) to_rank[j] = place[there ? e : 0];
-                    if (!there) idx[n][j] = -1;
+                    const uint32_t e = min(static_cast<uint32_t>(idx[n][j]), static_cast<uint32_t>(E));
+                    atomicAdd(&bins[(e << log_copies) + copy], 1);
+                    if (R) rank[j] = place[e];
                 }
                 if (R) {
 #pragma unroll
                     for (int j = 1; j < K; ++j) {
                         bool again = false;
 #pragma unroll
-                        for (int i = 0; i < j; ++i) again = again || (to_rank[i] == to_rank[j] && idx[n][i] >= 0);
-                        if (again && idx[n][j] >= 0 && static_cast<uint32_t>(to_rank[j]) < static_cast<uint32_t>(R))
-                            atomicAdd(&dups[to_rank[j] * dup_copies + dup_copy], 1);
+                        for (int i = 0; i < j; ++i) again = again | (rank[i] == rank[j]);
+                        if (again && rank[j] >= 0) atomicAdd(&dups[(rank[j] << log_dups) + dup_copy], 1);
                     }
                 }
             }
@@ -205,15 +211,15 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int copies,
         int32_t *part = a.part + (static_cast<int64_t>(blockIdx.x) + s) * M;
         for (int e = threadIdx.x; e < E; e += kCountBlock) {
             int t = 0;
-            for (int c = 0; c < copies; ++c) t += bins[e * copies + ((c + e) & (copies - 1))];
+            for (int c = 0; c < copies; ++c) t += bins[(e << log_copies) + ((c + e) & (copies - 1))];
             if (a.counts) part[e] = t;
-            if (R && static_cast<uint32_t>(place[e]) < static_cast<uint32_t>(R)) atomicAdd(&totals[place[e]], t);
+            if (R && place[e] >= 0) atomicAdd(&totals[place[e]], t);
         }
         if (R) {
             __syncthreads();
             for (int r = threadIdx.x; r < R; r += kCountBlock) {
                 int t = totals[r];
-                for (int c = 0; c < dup_copies; ++c) t -= dups[r * dup_copies + ((c + r) & (dup_copies - 1))];
+                for (int c = 0; c < dup_copies; ++c) t -= dups[(r << log_dups) + ((c + r) & (dup_copies - 1))];
                 part[M - R + r] = t;
             }
         }
@@ -338,14 +344,14 @@ hipError_t counts_of(const CountArgs &a, hipStream_t stream)
 {
     // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
     // workgroups to a CU at the largest sizes; and no more bins than a chunk has slots
-    int copies = 32, dup_copies = 8;
+    int log_copies = 5, log_dups = 3;
     const int64_t slots = std::min<int64_t>(static_cast<int64_t>(a.rows.chunk) * K, 8192);
-    while (copies > 1 && a.experts * copies > slots) copies /= 2;
-    while (dup_copies > 1 && a.ranks * dup_copies > 2048) dup_copies /= 2;
-    const int R = a.rank_tokens ? a.ranks : 0;
-    const size_t lds = sizeof(int) * (static_cast<size_t>(a.experts) * (copies + 1) + R * (dup_copies + 1));
+    while (log_copies > 0 && static_cast<int64_t>(a.experts) << log_copies > slots) --log_copies;
+    while (log_dups > 0 && static_cast<int64_t>(a.ranks) << log_dups > 2048) --log_dups;
+    const size_t R = a.rank_tokens ? a.ranks : 0, bins = a.experts + 1;
+    const size_t lds = sizeof(int) * ((bins << log_copies) + bins + (R << log_dups) + R);
     const bool aligned = reinterpret_cast<uintptr_t>(a.index) % 16 == 0;
-    k_counts<K><<<a.rows.chunks, kCountBlock, lds, stream>>>(a, copies, dup_copies, aligned);
+    k_counts<K><<<a.rows.chunks, kCountBlock, lds, stream>>>(a, log_copies, log_dups, aligned);
     return hipGetLastError();
 }
 

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
             if (r0 != ahead_of)
                 ahead.load(logits + row * a.stride, a.experts, l, shape);
-            const RowOf<D, L, V> raw = ahead;
+            RowOf<D, L, V> raw = ahead;
             const int64_t slot = row * a.top_k + min(l, a.top_k - 1);   // (lanes without a slot read the last)
             int index = a.index[slot];
             float w = a.weight[slot], gw = a.grad_weight ? a.grad_weight[slot] : 0.0f;
@@ -92,6 +92,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             const float slope = w * ((there ? gw : 0.0f) - (renorm ? all * per_scale : 0.0f));
             if (index >= 0 && inside) atomicAdd(&mine[index], slope);
             float x[V], sum = 0.0f, rest = 0.0f, r[V];
+            raw.end_at(a.experts, l, shape);
             raw.values(x);
             float top = x[0];
 #pragma unroll

@@ -301,27 +301,16 @@ struct RowOf {
     }
     __device__ __forceinline__ void load(const typename D::Raw *row, int experts, int l, int shape)
     {
-        constexpr int kWordsOfRun = kRun / kPer;
         const int at = anew(l * kRun);
         if (shape == kFull) {
 #pragma unroll
             for (int q = 0; q < V / kRun; ++q)
                 put(q, *reinterpret_cast<const Run<D, kRun> *>(row + q * (L * kRun) + at));
         } else if (shape == kWhole) {
-            Run<D, kRun> r[V / kRun];
 #pragma unroll
             for (int q = 0; q < V / kRun; ++q) {
                 const int col = q * (L * kRun) + at;
-                r[q] = *reinterpret_cast<const Run<D, kRun> *>(row + (col < experts ? col : 0));
-            }
-#pragma unroll
-            for (int q = 0; q < V / kRun; ++q) {
-                put(q, r[q]);
-#pragma unroll
-                for (int i = 0; i < kWordsOfRun; ++i) {
-                    const uint32_t w = word[q * kWordsOfRun + i];
-                    word[q * kWordsOfRun + i] = q * (L * kRun) + at < experts ? w : none();
-                }
+                put(q, *reinterpret_cast<const Run<D, kRun> *>(row + (col < experts ? col : 0)));
             }
         } else {
             typename D::Raw r[V];
@@ -341,6 +330,15 @@ struct RowOf {
                 word[w] = v;
             }
         }
+    }
+    // What load() leaves of columns beyond the row's end, once the values are there: reading ahead does not
+    // wait for them.
+    __device__ __forceinline__ void end_at(int experts, int l, int shape)
+    {
+        if (shape != kWhole) return;
+        const int at = anew(l * kRun);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) word[w] = column_of<L>(w * kPer) - w * kPer % kRun + at < experts ? word[w] : none();
     }
     __device__ __forceinline__ void drop(bool keep)
     {

@@ -300,6 +300,7 @@ __global__ __launch_bounds__(kRowWaves *kWave, waves_per_simd(V)) void k_route(R
                 ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, to - 1)) * a.stride, a.experts, l, shape);
             }
             const bool live = inside && (!a.keep || a.keep[row] != 0);
+            raw.end_at(a.experts, l, shape);
             if (__ballot(live) != ~0ull) raw.drop(live);
             float x[V], logit, top = 0.0f;
             int index;
