@@ -89,22 +89,24 @@ __global__ __launch_bounds__(COLS *ROWS) void k_route_finish(RouteArgs a)
 
 // ---- loss ------------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void k_balance_loss(int experts, double unit, const int32_t *counts,
-                                                      const int32_t *routed, const float *prob_sum,
-                                                      float *loss)
+// A workgroup per segment, of up to 1024 threads: all reads are under way at once.
+__global__ __launch_bounds__(1024) void k_balance_loss(int experts, double unit, const int32_t *counts,
+                                                       const int32_t *routed, const float *prob_sum,
+                                                       float *loss)
 {
-    __shared__ double part[4];
+    __shared__ double part[1024 / kWave];
     const int64_t at = static_cast<int64_t>(blockIdx.x) * experts;
+    const int rows = routed[blockIdx.x];
     double t = 0.0;
-    for (int e = threadIdx.x; e < experts; e += 256)
+    for (int e = threadIdx.x; e < experts; e += blockDim.x)
         t = t + static_cast<double>(counts[at + e]) * static_cast<double>(prob_sum[at + e]);
     for (int step = 1; step < kWave; step *= 2) t = t + __shfl_xor(t, step, kWave);
     if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = t;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const double n = static_cast<double>(routed[blockIdx.x]);
-        t = ((part[0] + part[1]) + part[2]) + part[3];
-        loss[blockIdx.x] = routed[blockIdx.x] == 0 ? 0.0f : static_cast<float>(unit * t / (n * n));
+        const double n = static_cast<double>(rows);
+        for (int w = 1; w < static_cast<int>(blockDim.x) / kWave; ++w) t = t + part[w];
+        loss[blockIdx.x] = rows == 0 ? 0.0f : static_cast<float>(unit * t / (n * n));
     }
 }
 
@@ -325,7 +327,8 @@ hipError_t launch_balance_loss(int32_t segments, int32_t experts, int32_t top_k,
                                const float *prob_sum, float alpha, float *loss, hipStream_t stream)
 {
     const double unit = static_cast<double>(alpha) * experts / top_k;
-    k_balance_loss<<<segments, 256, 0, stream>>>(experts, unit, counts, routed, prob_sum, loss);
+    const int threads = std::min(1024, round_up(experts, kWave));
+    k_balance_loss<<<segments, threads, 0, stream>>>(experts, unit, counts, routed, prob_sum, loss);
     return hipGetLastError();
 }
 
