@@ -14,7 +14,7 @@ namespace {
 
 namespace moe = nimble::moe;
 
-constexpr int32_t kChunks = 1 << 20, kChunksOfSums = 1 << 9, kChunksOfGradient = 1 << 9;
+constexpr int32_t kChunks = 1 << 13, kChunksOfSums = 1 << 9, kChunksOfGradient = 1 << 9;
 
 nimble_status_t bad(const char *what) { return report(NIMBLE_ERR_INVALID, what); }
 nimble_status_t too_large(const char *what) { return report(NIMBLE_ERR_RANGE, what); }

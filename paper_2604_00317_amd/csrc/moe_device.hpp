@@ -164,12 +164,12 @@ __device__ __forceinline__ float sigmoid_of(float x)
     return __builtin_amdgcn_rcpf(1.0f + exp_of(-x));
 }
 
-// exp(x - shift) up to a factor that is the same for all x (the rounding of `at`, shift * log2(e)), in a
-// multiply-add and an exp2.  Where `at` is not finite there is no such factor, and far() says so.
+// exp(x - shift) up to a factor that is the same for all x (2 to the rounding of `at`, shift * log2(e)), in a
+// multiply-add and an exp2.  far(): `at` is so large that the factor may leave the range, or no number.
 struct Shifted {
     float shift, at;
     __device__ __forceinline__ explicit Shifted(float s) : shift(s), at(s * kLog2E) {}
-    __device__ __forceinline__ bool far() const { return fabsf(at) == kInf; }
+    __device__ __forceinline__ bool far() const { return !(fabsf(at) <= 16777216.0f); }
     __device__ __forceinline__ float near_exp(float x) const
     {
         return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2E, -at));

@@ -243,6 +243,29 @@ def test_rows_at_the_edges(B, dtype, sigmoid, E):
         assert not got["grad"][0].any() and not got["grad"][10].any() and not got["grad"][20].any()
 
 
+@pytest.mark.parametrize("offset", [0.0, -70.0, 1e5, 2e7, -2e7, 1e9, -1e9, 1e20, -3e38, 3e38])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_far_from_zero(B, offset, dtype):
+    """Softmax does not depend on what all logits of a row have in common, however much that is.  (The
+    logits that are left of the sum are steps of the type: the definition is taken of them.)"""
+    import torch
+    rng = np.random.default_rng(17)
+    T, E, k = 12, 90, 5
+    with np.errstate(over="ignore"):
+        x = (rng.normal(size=(T, E)) * 2).astype(np.float32) + np.float32(offset)
+    x[3] = rng.normal(size=E)                          # an ordinary row in the same wave
+    d = torch.as_tensor(x).to("cuda:0", getattr(torch, dtype))
+    x = d.float().cpu().numpy()
+    for sigmoid in (False, True):
+        for renorm in (False, True):
+            kw = dict(sigmoid=sigmoid, renorm=renorm, grad_weight=rng.normal(size=(T, k)).astype(np.float32),
+                      grad_loss=np.ones(1, dtype=np.float32), alpha=0.5)
+            got = run(B, d, k, backward=True, **kw)
+            check(got, x, k, dtype, **kw)
+            served = run(B, d, k, sums=False, sigmoid=sigmoid, renorm=renorm)
+            assert np.array_equal(served["index"], got["index"])
+
+
 def test_a_bias_that_excludes_and_one_that_forces(B):
     import torch
     rng = np.random.default_rng(9)
