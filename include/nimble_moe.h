@@ -44,6 +44,7 @@ extern "C" {
 
 /* limits (NIMBLE_ERR_RANGE beyond them) */
 enum {
+    NIMBLE_MOE_MAX_TOKENS = 0x7FFF0000,
     NIMBLE_MOE_MAX_EXPERTS = 2048,
     NIMBLE_MOE_MAX_TOP_K = 16,
     NIMBLE_MOE_MAX_RANKS = 4096,
@@ -85,7 +86,7 @@ enum { NIMBLE_MOE_WAY_BACK = 1u /* the demand of the way back: destination to so
  *   d_bias       float [experts], or NULL; NaN counts as -inf, +inf as the largest finite number
  *   d_keep       [tokens], 0 for rows to leave out (padding): they have no choice and may hold
  *                anything; or NULL
- *   scale        finite and > 0
+ *   scale        finite and > 0 (and no denormal number)
  *   d_index      int32 [tokens][top_k] out
  *   d_weight     float [tokens][top_k] out
  *   d_counts     int32 [n_segments][experts] out   \

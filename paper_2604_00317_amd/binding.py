@@ -483,7 +483,7 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
                      scale: float = 1.0, d_bias=None, d_keep=None, d_seg_ptr=None, d_counts=None,
                      d_routed=None, d_prob_sum=None, d_scratch=None, stream=None) -> None:
     """Chooses d_index.shape[1] experts per row of d_logits [tokens][experts] (float32, float16 or
-    bfloat16; rows may be strided), with their weights.  d_counts [segments][experts], d_routed
+    bfloat16; rows may be strided), with their weights.  d_keep is uint8 or bool.  d_counts [segments][experts], d_routed
     [segments] and d_prob_sum [segments][experts] are wanted together or not at all."""
     lib = _lib or load_library()
     i32, f32 = _torch.int32, _torch.float32
@@ -496,7 +496,8 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
     if d_bias is not None:
         bias = _moe_ptr(d_bias, f32, experts, gpu, "d_bias")
     if d_keep is not None:
-        keep = _moe_ptr(d_keep, _torch.uint8, tokens, gpu, "d_keep")
+        keep = _moe_ptr(d_keep, _torch.bool if d_keep.dtype is _torch.bool else _torch.uint8, tokens,
+                        gpu, "d_keep")
     if d_counts is not None:
         counts = _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts")
         scratch, nbytes, owner = _moe_scratch(
@@ -550,7 +551,8 @@ def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sig
         n_seg = d_seg_ptr.numel() - 1
         seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
     if d_keep is not None:
-        keep = _moe_ptr(d_keep, _torch.uint8, tokens, gpu, "d_keep")
+        keep = _moe_ptr(d_keep, _torch.bool if d_keep.dtype is _torch.bool else _torch.uint8, tokens,
+                        gpu, "d_keep")
     if d_grad_weight is not None:
         grad_weight = _moe_ptr(d_grad_weight, f32, tokens * top_k, gpu, "d_grad_weight")
     if d_counts is not None:

@@ -26,6 +26,8 @@ nimble_status_t check_sizes(int32_t tokens, int32_t experts, int32_t top_k)
     if (top_k < 1) return bad("top_k must be >= 1");
     if (experts > NIMBLE_MOE_MAX_EXPERTS) return too_large("more than 2048 experts");
     if (top_k > NIMBLE_MOE_MAX_TOP_K) return too_large("top_k is more than 16");
+    // (row numbers a pass beyond the last one fit 32 bits)
+    if (tokens > NIMBLE_MOE_MAX_TOKENS) return too_large("more than 2^31 - 2^16 tokens");
     return NIMBLE_OK;
 }
 
@@ -70,7 +72,7 @@ nimble_status_t check_route(uint32_t flags, int32_t dtype, int32_t experts, int3
     if (dtype != NIMBLE_F32 && dtype != NIMBLE_F16 && dtype != NIMBLE_BF16) return bad("unknown dtype");
     if (top_k > experts) return bad("top_k is more than the number of experts");
     if (row_stride < experts) return bad("row_stride is less than the number of experts");
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return bad("scale must be finite and > 0");
+    if (!(scale > 0.0f) || !std::isnormal(scale)) return bad("scale must be finite, > 0 and no denormal number");
     return NIMBLE_OK;
 }
 
@@ -78,8 +80,8 @@ nimble_status_t check_route(uint32_t flags, int32_t dtype, int32_t experts, int3
 
 int64_t nimble_moe_route_scratch_bytes(int32_t tokens, int32_t experts, int32_t n_segments)
 {
-    if (tokens < 0 || experts < 1 || experts > NIMBLE_MOE_MAX_EXPERTS || n_segments < 1 ||
-        n_segments > NIMBLE_MOE_MAX_SEGMENTS)
+    if (tokens < 0 || tokens > NIMBLE_MOE_MAX_TOKENS || experts < 1 || experts > NIMBLE_MOE_MAX_EXPERTS ||
+        n_segments < 1 || n_segments > NIMBLE_MOE_MAX_SEGMENTS)
         return -1;
     const int32_t chunk = moe::route_chunk(tokens, experts, kChunksOfSums);
     return 2 * part_bytes(tokens, chunk, n_segments, experts) + part_bytes(tokens, chunk, n_segments, 1);
@@ -205,7 +207,7 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
 int64_t nimble_moe_counts_scratch_bytes(int32_t tokens, int32_t top_k, int32_t experts,
                                         int32_t n_ranks, int32_t n_segments)
 {
-    if (tokens < 0 || top_k < 1 || top_k > NIMBLE_MOE_MAX_TOP_K || experts < 1 ||
+    if (tokens < 0 || tokens > NIMBLE_MOE_MAX_TOKENS || top_k < 1 || top_k > NIMBLE_MOE_MAX_TOP_K || experts < 1 ||
         experts > NIMBLE_MOE_MAX_EXPERTS || n_ranks < 0 || n_ranks > NIMBLE_MOE_MAX_RANKS ||
         n_segments < 1 || n_segments > NIMBLE_MOE_MAX_SEGMENTS)
         return -1;

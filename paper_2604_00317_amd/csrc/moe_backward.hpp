@@ -30,11 +30,13 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
     float *mine = slots[wave * G + g];
 #pragma unroll
     for (int j = 0; j < V; ++j) mine[column_of<L>(j) + l * kRun] = 0.0f;
-    // Rows are read a pass ahead; the first ones before it is known which segment they are in.
+    // Rows are read a pass ahead; the first ones before it is known which segment they are in.  Divided softmax
+    // weights alone have a gradient that the weights give: no logits are read for it.
+    const bool dense = a.counts || sigmoid || !renorm;
     const auto *const logits = static_cast<const typename D::Raw *>(a.logits);
-    RowOf<D, L, V> ahead;
+    RowOf<D, L, V> ahead{};
     int ahead_of = lo + wave * G;
-    ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, hi - 1)) * a.stride, a.experts, l, shape);
+    if (dense) ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, hi - 1)) * a.stride, a.experts, l, shape);
     Segments segments(a.rows, lane);
     for (int s = segments.first(lo); s < a.rows.segments; ++s) {
         const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
         for (int r0 = from + wave * G; r0 < to; r0 += kRowWaves * G) {
             const bool inside = r0 + g < to;
             const int64_t row = inside ? r0 + g : to - 1;       // (no group reads outside the part)
-            if (r0 != ahead_of)
+            if (dense && r0 != ahead_of)
                 ahead.load(logits + row * a.stride, a.experts, l, shape);
             RowOf<D, L, V> raw = ahead;
             const int64_t slot = row * a.top_k + min(l, a.top_k - 1);   // (lanes without a slot read the last)
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             float w = a.weight[slot], gw = a.grad_weight ? a.grad_weight[slot] : 0.0f;
             if (r0 + kRowWaves * G < to) {
                 ahead_of = r0 + kRowWaves * G;
-                ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, to - 1)) * a.stride, a.experts, l, shape);
+                if (dense) ahead.load(logits + static_cast<int64_t>(min(ahead_of + g, to - 1)) * a.stride, a.experts, l, shape);
             }
             const bool kept = !a.keep || a.keep[row] != 0;
             const bool nan = kept && l == 0 && !(w == w);

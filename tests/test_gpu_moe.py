@@ -328,6 +328,18 @@ def test_row_counts_and_segments(B, T, S):
     assert np.array_equal(served["weight"], got["weight"], equal_nan=True)
 
 
+def test_a_mask_of_truth_values(B):
+    import torch
+    rng = np.random.default_rng(5)
+    x = logits(rng, 40, 32, "float32")
+    keep = rng.random(40) < 0.5
+    ref = run(B, x, 3, keep=keep)
+    idx = torch.full((40, 3), -2, dtype=torch.int32, device="cuda:0")
+    w = torch.zeros((40, 3), device="cuda:0")
+    B.nimble_moe_route(x, idx, w, d_keep=torch.as_tensor(keep).to("cuda:0"))
+    assert np.array_equal(idx.cpu().numpy(), ref["index"]) and np.array_equal(w.cpu().numpy(), ref["weight"])
+
+
 def test_offsets_out_of_range_are_cut(B):
     rng = np.random.default_rng(1)
     x = logits(rng, 20, 16, "float32")

@@ -114,7 +114,8 @@ SUMS = dict(ROUTE, counts=P, routed=P, prob=P, scratch=P, nbytes=1 << 20)
     (ROUTE, dict(flags=4), 1), (ROUTE, dict(dtype=3), 1), (ROUTE, dict(dtype=-1), 1),
     (ROUTE, dict(logits=None), 1), (ROUTE, dict(index=None), 1), (ROUTE, dict(weight=None), 1),
     (ROUTE, dict(stride=7), 1), (ROUTE, dict(scale=0.0), 1), (ROUTE, dict(scale=float("nan")), 1),
-    (ROUTE, dict(scale=float("inf")), 1), (ROUTE, dict(scale=-1.0), 1), (ROUTE, dict(n_seg=0), 1),
+    (ROUTE, dict(scale=float("inf")), 1), (ROUTE, dict(scale=1e-39), 1), (ROUTE, dict(tokens=0x7FFF0001), 4),
+    (ROUTE, dict(scale=-1.0), 1), (ROUTE, dict(n_seg=0), 1),
     (ROUTE, dict(n_seg=2), 1), (ROUTE, dict(n_seg=(1 << 20) + 1, seg=P), 4),
     (ROUTE, dict(counts=P), 1), (SUMS, dict(prob=None), 1), (SUMS, dict(scratch=None), 1),
     (SUMS, dict(scratch=ctypes.c_void_p(4100)), 1), (SUMS, dict(nbytes=16), 1),
@@ -145,7 +146,7 @@ BACK = dict(tokens=4, experts=8, top_k=2, flags=0, dtype=0, logits=P, stride=8, 
     (dict(tokens=-1), 1), (dict(top_k=9), 1), (dict(flags=8), 1), (dict(dtype=5), 1), (dict(stride=7), 1),
     (dict(gstride=7), 1), (dict(logits=None), 1), (dict(index=None), 1), (dict(weight=None), 1),
     (dict(grad=None), 1), (dict(counts=None), 1), (dict(routed=None), 1),
-    (dict(gl=None), 1), (dict(alpha=float("nan")), 1), (dict(scale=0.0), 1), (dict(n_seg=3), 1),
+    (dict(gl=None), 1), (dict(scale=1e-39), 1), (dict(tokens=0x7FFFFFFF), 4), (dict(alpha=float("nan")), 1), (dict(scale=0.0), 1), (dict(n_seg=3), 1),
     (dict(experts=4000, stride=4000, gstride=4000), 4)])
 def test_backward_refuses(change, status):
     assert B.load_library().nimble_moe_route_backward(*dict(BACK, **change).values()) == status
@@ -157,6 +158,7 @@ COUNT = dict(tokens=4, top_k=2, index=P, experts=8, n_seg=1, seg=None, place=P, 
 
 @pytest.mark.parametrize("change,status", [
     (dict(tokens=-1), 1), (dict(top_k=0), 1), (dict(top_k=17), 4), (dict(experts=0), 1),
+    (dict(tokens=0x7FFF0001), 4),
     (dict(experts=2049), 4), (dict(index=None), 1), (dict(n_seg=0), 1), (dict(n_seg=2), 1),
     (dict(counts=None, rank_tokens=None), 1), (dict(place=None), 1), (dict(ranks=0), 1),
     (dict(ranks=-1), 1), (dict(ranks=4097), 4), (dict(scratch=None), 1), (dict(nbytes=8), 1)])
@@ -182,8 +184,10 @@ def test_scratch_sizes():
     assert B.nimble_moe_route_scratch_bytes(-1, 8) == -1 == B.nimble_moe_route_scratch_bytes(4, 4096)
     assert B.nimble_moe_route_scratch_bytes(4, 8, 0) == -1
     assert B.nimble_moe_counts_scratch_bytes(4, 17, 8) == -1 == B.nimble_moe_counts_scratch_bytes(4, 2, 8, -1)
-    big = B.nimble_moe_route_scratch_bytes((1 << 31) - 1, 2048, 1 << 20)
-    assert big > 1 << 32 and B.nimble_moe_counts_scratch_bytes((1 << 31) - 1, 16, 2048, 4096, 1 << 20) > 1 << 32
+    most = 0x7FFF0000
+    big = B.nimble_moe_route_scratch_bytes(most, 2048, 1 << 20)
+    assert big > 1 << 32 and B.nimble_moe_counts_scratch_bytes(most, 16, 2048, 4096, 1 << 20) > 1 << 32
+    assert B.nimble_moe_route_scratch_bytes(most + 1, 8) == -1 == B.nimble_moe_counts_scratch_bytes(most + 1, 2, 8)
 
 
 def test_binding_refuses_host_tensors():
