@@ -163,6 +163,10 @@ __device__ __forceinline__ Choice choose(int (&key)[V], int top_k, int l)
 {
     constexpr int N = V < KL ? V : KL;
     largest<N, 0, V>(key);
+    // (the lists are done here: the compiler would put off their last steps into the slots that need them, and
+    // keep twice the registers until then)
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = anew(key[i]);
     Choice c{NONE, NONE, false, false};
     take<L, V, KL, N, 0, ROUNDED, NONE>(key, top_k, ((L - 1) ^ l) * kRun, 0, c);    // (the lane's part of the column)
     return c;

@@ -405,6 +405,35 @@ def test_offsets_beyond_32_bits(B):
     check(got, x.float().cpu().numpy(), k, "bfloat16", **kw)
 
 
+def test_more_than_2_to_the_31_slots(B):
+    """2^28 rows of eight slots: every array of slots passes 2^31 elements."""
+    import torch
+    T, E, k = (1 << 28) + 5, 8, 8
+    dev = "cuda:0"
+    pattern = torch.tensor([0.0, 3.0, -1.0, 7.0, 2.0, 2.0, -4.0, 5.0])
+    x = pattern.to(dev, torch.bfloat16).expand(T, E).contiguous()
+    last = torch.arange(E, dtype=torch.float32)
+    x[-1] = last.to(dev, torch.bfloat16)
+    index = torch.full((T, k), -2, dtype=torch.int32, device=dev)
+    weight = torch.full((T, k), math.nan, device=dev)
+    c = torch.zeros((2, E), dtype=torch.int32, device=dev)
+    r = torch.zeros(2, dtype=torch.int32, device=dev)
+    p = torch.zeros((2, E), device=dev)
+    seg = torch.tensor([0, T - 1, T], dtype=torch.int32, device=dev)
+    B.nimble_moe_route(x, index, weight, d_seg_ptr=seg, d_counts=c, d_routed=r, d_prob_sum=p)
+    ref = M.route(np.stack([pattern.numpy(), last.numpy()]), k, ends=[0, 1, 2])
+    assert (index[:-1] == index[0]).all() and (weight[:-1] == weight[0]).all()
+    assert index[[0, -1]].cpu().numpy().tolist() == ref["index"].tolist()
+    np.testing.assert_allclose(weight[[0, -1]].cpu().numpy(), ref["weight"], rtol=float(rel(pattern.numpy()[None])[0]))
+    assert c.tolist() == [[T - 1] * E, [1] * E] and r.tolist() == [T - 1, 1]
+    del weight, x
+    counts = torch.zeros((2, E), dtype=torch.int32, device=dev)
+    tokens = torch.zeros((2, 3), dtype=torch.int32, device=dev)
+    place = torch.tensor([0, 0, 0, 1, 1, 1, 1, 1], dtype=torch.int32, device=dev)
+    B.nimble_moe_counts(index, E, counts, d_expert_rank=place, d_rank_tokens=tokens, d_seg_ptr=seg)
+    assert counts.tolist() == c.tolist() and tokens.tolist() == [[T - 1, T - 1, 0], [1, 1, 0]]
+
+
 # ---- counts and demand -----------------------------------------------------------------------
 
 def gpu_counts(B, index, E, seg=None, place=None, ranks=0, counts=True):
