@@ -52,6 +52,7 @@ EXPORTS = [
 _lib = None
 _torch = None               # the module, once the library is loaded
 _MOE_KINDS = {}             # element types of logits
+_current_gpu = _raw_stream = None   # torch's own, without its checks
 
 
 class NimbleError(RuntimeError):
@@ -62,7 +63,7 @@ class NimbleError(RuntimeError):
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     """Loads the in-tree library; builds it first only when no built library exists."""
-    global _lib, _torch
+    global _lib, _torch, _current_gpu, _raw_stream
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -76,6 +77,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     # round, torch finds a runtime it was not built for and reports no GPU).
     import torch
     _torch = torch
+    _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _MOE_KINDS.update({torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16,
                        torch.bfloat16: NIMBLE_BF16})
     lib = ctypes.CDLL(LIB_PATH)
@@ -445,7 +448,7 @@ def _moe_gpu(t, what):
 
 def _moe_stream(stream, gpu):
     if stream is None:
-        return _torch._C._cuda_getCurrentRawStream(gpu)
+        return _raw_stream(gpu)
     if stream.device.index != gpu:
         raise ValueError("the stream is on another GPU than the tensors")
     return stream.cuda_stream
@@ -469,14 +472,9 @@ def _moe_scratch(t, nbytes, gpu, stream):
     return t.data_ptr(), t.numel() * t.element_size(), t
 
 
-def _moe_run(gpu, fn, *args):
-    if _torch._C._cuda_getDevice() == gpu:
-        status = fn(*args)
-    else:
-        with _torch.cuda.device(gpu):
-            status = fn(*args)
-    if status:
-        raise NimbleError(status, nimble_last_error())
+def _moe_elsewhere(gpu, fn, args):
+    with _torch.cuda.device(gpu):
+        return fn(*args)
 
 
 def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, renorm: bool = True,
@@ -506,12 +504,16 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
         routed = _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed")
     if d_prob_sum is not None:
         prob = _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum")
-    _moe_run(gpu, lib.nimble_moe_route, tokens, experts, top_k,
-             (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
-             stride, bias, keep, scale, n_seg, seg,
-             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
-             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), counts, routed, prob, scratch,
-             nbytes, _moe_stream(stream, gpu))
+    args = (tokens, experts, top_k,
+            (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
+            stride, bias, keep, scale, n_seg, seg,
+            _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
+            _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), counts, routed, prob, scratch,
+            nbytes, _moe_stream(stream, gpu))
+    fn = lib.nimble_moe_route
+    status = fn(*args) if _current_gpu() == gpu else _moe_elsewhere(gpu, fn, args)
+    if status:
+        raise NimbleError(status, nimble_last_error())
 
 
 def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 1) -> int:
@@ -527,11 +529,15 @@ def nimble_moe_balance_loss(d_counts, d_routed, d_prob_sum, top_k: int, alpha: f
     if d_counts.dim() != 2:
         raise ValueError("d_counts must be [segments][experts]")
     n_seg, experts = d_counts.shape
-    _moe_run(gpu, lib.nimble_moe_balance_loss, n_seg, experts, top_k,
-             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
-             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
-             _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum"), alpha,
-             _moe_ptr(d_loss, f32, n_seg, gpu, "d_loss"), _moe_stream(stream, gpu))
+    args = (n_seg, experts, top_k,
+            _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
+            _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
+            _moe_ptr(d_prob_sum, f32, n_seg * experts, gpu, "d_prob_sum"), alpha,
+            _moe_ptr(d_loss, f32, n_seg, gpu, "d_loss"), _moe_stream(stream, gpu))
+    fn = lib.nimble_moe_balance_loss
+    status = fn(*args) if _current_gpu() == gpu else _moe_elsewhere(gpu, fn, args)
+    if status:
+        raise NimbleError(status, nimble_last_error())
 
 
 def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sigmoid: bool = False,
@@ -561,12 +567,16 @@ def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sig
         routed = _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed")
     if d_grad_loss is not None:
         grad_loss = _moe_ptr(d_grad_loss, f32, n_seg, gpu, "d_grad_loss")
-    _moe_run(gpu, lib.nimble_moe_route_backward, tokens, experts, top_k,
-             (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
-             stride, keep, scale, n_seg, seg,
-             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
-             _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), grad_weight, alpha, counts,
-             routed, grad_loss, dx, grad_stride, _moe_stream(stream, gpu))
+    args = (tokens, experts, top_k,
+            (NIMBLE_MOE_SIGMOID if sigmoid else 0) | (NIMBLE_MOE_RENORM if renorm else 0), kind, x,
+            stride, keep, scale, n_seg, seg,
+            _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"),
+            _moe_ptr(d_weight, f32, tokens * top_k, gpu, "d_weight"), grad_weight, alpha, counts,
+            routed, grad_loss, dx, grad_stride, _moe_stream(stream, gpu))
+    fn = lib.nimble_moe_route_backward
+    status = fn(*args) if _current_gpu() == gpu else _moe_elsewhere(gpu, fn, args)
+    if status:
+        raise NimbleError(status, nimble_last_error())
 
 
 def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=None,
@@ -594,9 +604,13 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
     scratch, nbytes, owner = _moe_scratch(
         d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg), gpu,
         stream)
-    _moe_run(gpu, lib.nimble_moe_counts, tokens, top_k,
-             _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"), experts, n_seg, seg, place,
-             ranks, counts, rank_tokens, scratch, nbytes, _moe_stream(stream, gpu))
+    args = (tokens, top_k,
+            _moe_ptr(d_index, i32, tokens * top_k, gpu, "d_index"), experts, n_seg, seg, place,
+            ranks, counts, rank_tokens, scratch, nbytes, _moe_stream(stream, gpu))
+    fn = lib.nimble_moe_counts
+    status = fn(*args) if _current_gpu() == gpu else _moe_elsewhere(gpu, fn, args)
+    if status:
+        raise NimbleError(status, nimble_last_error())
 
 
 def nimble_moe_counts_scratch_bytes(tokens: int, top_k: int, experts: int, n_ranks: int = 0,
@@ -621,11 +635,15 @@ def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traf
         src = _moe_ptr(d_src, i32, n_comm, gpu, "d_src")
     if d_dst is not None:
         dst = _moe_ptr(d_dst, i32, n_comm, gpu, "d_dst")
-    _moe_run(gpu, lib.nimble_moe_traffic, batch, ranks,
-             _moe_ptr(d_rank_tokens, i32, batch * ranks * ranks, gpu, "d_rank_tokens"),
-             bytes_per_token, n_comm, src, dst, NIMBLE_MOE_WAY_BACK if way_back else 0,
-             _moe_ptr(d_traffic, _torch.float64, batch * n_comm, gpu, "d_traffic"),
-             _moe_stream(stream, gpu))
+    args = (batch, ranks,
+            _moe_ptr(d_rank_tokens, i32, batch * ranks * ranks, gpu, "d_rank_tokens"),
+            bytes_per_token, n_comm, src, dst, NIMBLE_MOE_WAY_BACK if way_back else 0,
+            _moe_ptr(d_traffic, _torch.float64, batch * n_comm, gpu, "d_traffic"),
+            _moe_stream(stream, gpu))
+    fn = lib.nimble_moe_traffic
+    status = fn(*args) if _current_gpu() == gpu else _moe_elsewhere(gpu, fn, args)
+    if status:
+        raise NimbleError(status, nimble_last_error())
 
 
 def nimble_debug_run_phase(topo: Topo, phase: int, reps: int, d_traffic, stream=None) -> None:
