@@ -301,7 +301,7 @@ bool many_parts(const Rows &r) { return r.chunks > 8 * static_cast<int64_t>(r.se
 int32_t route_chunk(int32_t tokens, int32_t experts, int32_t most)
 {
     return round_up((static_cast<int64_t>(tokens) + most - 1) / most,
-                    kRowWaves * (experts <= 256 ? 4 : experts <= 512 ? 2 : 1));
+                    kRowWaves * (experts <= 128 ? 8 : experts <= 256 ? 4 : experts <= 512 ? 2 : 1));
 }
 
 int32_t count_chunk(int32_t tokens, int32_t) { return round_up((static_cast<int64_t>(tokens) + 1023) / 1024, kCountBlock); }

@@ -17,6 +17,7 @@ template <class D, int L, int V>
 __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArgs a, int shape)
 {
     constexpr int C = L * V, G = kWave / L;
+    constexpr int kSlots = L < 16 ? L : 16;              // lanes of a group that have slots
     __shared__ __align__(16) float slots[kRowWaves * G][C];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             index = there ? index : -1;
             w = there ? w : 0.0f;
             const float wg = there ? w * gw : 0.0f;
-            const float all = group_sum<16>(wg);
+            const float all = group_sum<kSlots>(wg);
             const float slope = w * ((there ? gw : 0.0f) - (renorm ? all * per_scale : 0.0f));
             if (index >= 0 && inside) atomicAdd(&mine[index], slope);
             float x[V], sum = 0.0f, rest = 0.0f, r[V];
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             }
             const float inv = 1.0f / group_sum<L>(sum);
             rest = group_sum<L>(rest) * inv;
-            // sums over the slots are in the first 16 lanes of a group
+            // sums over the slots are in the lanes that have them
             if (!sigmoid && !renorm) rest = rest + __shfl(all, lane & ~(L - 1));
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -164,6 +165,11 @@ hipError_t run(const BackwardArgs &a, hipStream_t stream)
 template <class D>
 hipError_t backward_rows(const BackwardArgs &a, hipStream_t stream)
 {
+    if (a.experts <= 128 && a.top_k <= 8) {
+        if (a.experts <= 32) return run<D, 8, 4>(a, stream);
+        if (a.experts <= 64) return run<D, 8, 8>(a, stream);
+        return run<D, 8, 16>(a, stream);
+    }
     if (a.experts <= 64) return run<D, 16, 4>(a, stream);
     if (a.experts <= 128) return run<D, 16, 8>(a, stream);
     if (a.experts <= 256) return run<D, 16, 16>(a, stream);

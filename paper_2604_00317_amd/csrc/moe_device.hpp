@@ -76,14 +76,14 @@ __device__ __forceinline__ float dpp_f32(float v)
     return float_of(dpp_i32<CTRL>(bits_of(v)));
 }
 
-// Over aligned groups of L lanes (16, 32 or 64); the same bits in all lanes of a group.
+// Over aligned groups of L lanes (8 to 64); the same bits in all lanes of a group.
 template <int L>
 __device__ __forceinline__ int group_max(int v)
 {
     v = max(v, dpp_i32<kDppXor1>(v));
     v = max(v, dpp_i32<kDppXor2>(v));
     v = max(v, dpp_i32<kDppHalfMirror>(v));
-    v = max(v, dpp_i32<kDppMirror>(v));
+    if constexpr (L > 8) v = max(v, dpp_i32<kDppMirror>(v));
     if constexpr (L > 16) {
         const TwoI32 r = both_rows(v);
         v = max(r.a, r.b);
@@ -108,7 +108,7 @@ __device__ __forceinline__ float group_max(float v)
     v = fmaxf(v, dpp_f32<kDppXor1>(v));
     v = fmaxf(v, dpp_f32<kDppXor2>(v));
     v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
-    v = fmaxf(v, dpp_f32<kDppMirror>(v));
+    if constexpr (L > 8) v = fmaxf(v, dpp_f32<kDppMirror>(v));
     if constexpr (L > 16) {
         const TwoI32 r = both_rows(bits_of(v));
         v = fmaxf(float_of(r.a), float_of(r.b));
@@ -125,7 +125,7 @@ __device__ __forceinline__ float group_sum(float v)
     v = v + dpp_f32<kDppXor1>(v);
     v = v + dpp_f32<kDppXor2>(v);
     v = v + dpp_f32<kDppHalfMirror>(v);
-    v = v + dpp_f32<kDppMirror>(v);
+    if constexpr (L > 8) v = v + dpp_f32<kDppMirror>(v);
     if constexpr (L > 16) {
         const TwoI32 r = both_rows(bits_of(v));
         v = float_of(r.a) + float_of(r.b);
@@ -136,10 +136,13 @@ __device__ __forceinline__ float group_sum(float v)
     }
     return v;
 }
+constexpr int kDppRotate8 = 0x128;                           // row_ror:8, the other half of a row of 16
+
 // The sum of a value over the groups of a wave, by lane of a group; the same bits in all groups.
 template <int L>
 __device__ __forceinline__ float over_groups(float v)
 {
+    if constexpr (L < 16) v = v + dpp_f32<kDppRotate8>(v);
     if constexpr (L < 32) {
         const TwoI32 r = both_rows(bits_of(v));
         v = float_of(r.a) + float_of(r.b);
@@ -256,7 +259,7 @@ private:
 
 // ---- rows in lanes ---------------------------------------------------------------------------
 
-// A row lies in a group of L lanes, V values per lane in runs of W neighbours (one load each): lane
+// A row lies in a group of L lanes (8 to 64), V values per lane in runs of W neighbours (one load each): lane
 // l of the group has columns q * L W + l W + 0 .. W-1 for q = 0 .. V/W - 1.  A wave holds 64/L rows.
 constexpr int kRun = 4;
 

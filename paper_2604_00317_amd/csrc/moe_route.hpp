@@ -1,6 +1,6 @@
 // Choice of experts, their weights, and the sums of the balance loss (include/nimble_moe.h).
 //
-// A row lies in a group of 16 to 64 lanes (moe_device.hpp), so a wave works on up to four rows at a
+// A row lies in a group of 8 to 64 lanes (moe_device.hpp), so a wave works on up to eight rows at a
 // time.  What bounds the kernel is the choice: everything else is half a dozen operations per logit.  It
 // is made of minima and maxima of 32-bit whole numbers, without branches:
 //   - a logit becomes a key whose order as a whole number is its order as a float, with the column, turned
@@ -257,6 +257,7 @@ template <class D, int L, int V, int KL, bool ROUNDED, bool SUMS>
 __global__ __launch_bounds__(kRowWaves *kWave, waves_per_simd(V)) void k_route(RouteArgs a, int shape)
 {
     constexpr int C = L * V, G = kWave / L, kCols = C - 1;
+    constexpr int kSlots = L < 16 ? L : 16;              // lanes of a group that have slots
     extern __shared__ float lds[];
     float *sums = lds;                                   // [kRowWaves][C]
     int *hits = reinterpret_cast<int *>(lds + kRowWaves * C);
@@ -380,9 +381,9 @@ __global__ __launch_bounds__(kRowWaves *kWave, waves_per_simd(V)) void k_route(R
             }
             float w;
             if (renorm) {
-                const float t = group_max<16>(logit);
+                const float t = group_max<kSlots>(logit);
                 const float u = score_of(sigmoid, logit, Shifted(shift_of(sigmoid, t)));
-                w = u * __builtin_amdgcn_rcpf(group_sum<16>(u));
+                w = u * __builtin_amdgcn_rcpf(group_sum<kSlots>(u));
             } else {
                 w = sigmoid ? sigmoid_of(logit) : by.exp(logit) * inv;
             }
@@ -452,23 +453,31 @@ hipError_t run(const RouteArgs &a, hipStream_t stream)
     return run<D, L, V, KL, true>(a, stream);
 }
 
+// Lists of one more than top_k where there are few: a lane that holds all the chosen ones of a row cannot
+// tell what comes next.
 template <class D, int L, int V>
 hipError_t run(const RouteArgs &a, hipStream_t stream)
 {
-    // lists of one more than top_k where there are few: a lane that holds all the chosen ones of a row
-    // cannot tell what comes next
+    if constexpr (L > 8)
+        if (a.top_k > 8) return run<D, L, V, 16>(a, stream);
     if (a.top_k <= 3) return run<D, L, V, 4>(a, stream);
-    if (a.top_k <= 8) return run<D, L, V, 8>(a, stream);
-    return run<D, L, V, 16>(a, stream);
+    return run<D, L, V, 8>(a, stream);
 }
 
 }  // namespace
 
+// Sixteen values to a lane where there are enough; as few lanes to a row as that makes, but as many as there
+// are slots.
 template <class D>
 hipError_t route_rows(const RouteArgs &a, hipStream_t stream)
 {
-    if (a.experts <= 64) return run<D, 16, 4>(a, stream);
-    if (a.experts <= 128) return run<D, 16, 8>(a, stream);
+    if (a.experts <= 128 && a.top_k <= 8) {
+        if (a.experts <= 32) return run<D, 8, 4>(a, stream);
+        if (a.experts <= 64) return run<D, 8, 8>(a, stream);
+        return run<D, 8, 16>(a, stream);
+    }
+    if (a.experts <= 64) return run<D, 16, 4, 16>(a, stream);
+    if (a.experts <= 128) return run<D, 16, 8, 16>(a, stream);
     if (a.experts <= 256) return run<D, 16, 16>(a, stream);
     if (a.experts <= 512) return run<D, 32, 16>(a, stream);
     if (a.experts <= 1024) return run<D, 64, 16>(a, stream);
