@@ -23,11 +23,12 @@ namespace {
 
 // The parts of segment s are p0 .. p1 (none: p1 < p0).
 struct Parts {
+    int lo, hi;                  // its rows
     int64_t p0, p1;
     __device__ __forceinline__ Parts(const Rows &r, int s)
     {
-        const int lo = r.seg_ptr ? min(max(r.seg_ptr[s], 0), r.tokens) : 0;
-        const int hi = r.seg_ptr ? min(max(r.seg_ptr[s + 1], 0), r.tokens) : r.tokens;
+        lo = r.seg_ptr ? min(max(r.seg_ptr[s], 0), r.tokens) : 0;
+        hi = r.seg_ptr ? min(max(r.seg_ptr[s + 1], 0), r.tokens) : r.tokens;
         p0 = static_cast<int64_t>(lo / r.chunk) + s;
         p1 = lo < hi ? static_cast<int64_t>((hi - 1) / r.chunk) + s : p0 - 1;
     }
@@ -120,100 +121,137 @@ __global__ __launch_bounds__(1024) void k_balance_loss(int experts, double unit,
 // end, less the slots that go where an earlier slot of the same row goes, which are few.
 constexpr int kCountBlock = 512;
 
+// Segments of up to kShort rows, whole, are counted by the workgroup that ends a segment (k_counts_segment), so
+// that thousands of short ones -- the tokens of every layer and source of a decoding step -- are not counted
+// one after the other by the few workgroups whose rows they are.
+constexpr int kShort = 512;
+
 // Rows a thread reads before it counts them.
 template <int K>
 constexpr int rows_at_once() { return K <= 4 ? 4 : K <= 8 ? 2 : 1; }
 
+// A thread's view of the bins in LDS.
+struct Bins {
+    int *experts;                // [experts + 1][copies]
+    int *dups;                   // [ranks][copies of theirs]
+    int log_copies, copy, log_dups, dup_copy;
+};
+
+// Counts rows from .. to-1, BLOCK of them at a time.  place_of(e), e <= experts, is the GPU of an expert, or
+// below 0, another for each, where it has none.
+template <int K, int BLOCK, class Place>
+__device__ __forceinline__ void count_rows(const CountArgs &a, bool aligned, int64_t from, int64_t to, bool ranks,
+                                           const Bins &bins, const Place &place_of)
+{
+    constexpr int N = rows_at_once<K>();
+    const uint32_t E = static_cast<uint32_t>(a.experts);
+    for (int64_t u0 = from; u0 < to; u0 += N * BLOCK) {
+        int idx[N][K];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (u0 + n * BLOCK >= to) break;
+            // (a row that is not there is read as the last one, and counts as no expert)
+            const int64_t row = u0 + n * BLOCK + threadIdx.x;
+            const int32_t *p = a.index + min(row, to - 1) * K;
+            if (K % 4 == 0 && aligned) {
+#pragma unroll
+                for (int j = 0; j + 3 < K; j += 4) {
+                    const int4 v = *reinterpret_cast<const int4 *>(p + j);
+                    idx[n][j] = v.x;
+                    idx[n][j + 1] = v.y;
+                    idx[n][j + 2] = v.z;
+                    idx[n][j + 3] = v.w;
+                }
+            } else if (K % 2 == 0 && aligned) {
+#pragma unroll
+                for (int j = 0; j + 1 < K; j += 2) {
+                    const int2 v = *reinterpret_cast<const int2 *>(p + j);
+                    idx[n][j] = v.x;
+                    idx[n][j + 1] = v.y;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < K; ++j) idx[n][j] = p[j];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (u0 + n * BLOCK >= to) break;
+            if (u0 + (n + 1) * BLOCK > to) {                         // the last rows
+                const bool inside = u0 + n * BLOCK + threadIdx.x < to;
+#pragma unroll
+                for (int j = 0; j < K; ++j) idx[n][j] = inside ? idx[n][j] : -1;
+            }
+            int rank[K];
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const uint32_t e = min(static_cast<uint32_t>(idx[n][j]), E);
+                atomicAdd(&bins.experts[(e << bins.log_copies) + bins.copy], 1);
+                if (ranks) rank[j] = place_of(e);
+            }
+            if (ranks) {
+#pragma unroll
+                for (int j = 1; j < K; ++j) {
+                    bool again = false;
+#pragma unroll
+                    for (int i = 0; i < j; ++i) again = again | (rank[i] == rank[j]);
+                    if (again && rank[j] >= 0) atomicAdd(&bins.dups[(rank[j] << bins.log_dups) + bins.dup_copy], 1);
+                }
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ int place_or_none(int r, int ranks, int e)
+{
+    return static_cast<uint32_t>(r) < static_cast<uint32_t>(ranks) ? r : -1 - e;
+}
+
 template <int K>
 __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_copies, int log_dups, bool aligned)
 {
-    constexpr int N = rows_at_once<K>();
     extern __shared__ int lds[];
     const int E = a.experts, R = a.rank_tokens ? a.ranks : 0;
-    int *bins = lds;                                 // [experts + 1][copies]
-    int *dups = bins + ((E + 1) << log_copies);      // [ranks][copies of theirs]
-    int *totals = dups + (R << log_dups);            // [ranks]
-    int *place = totals + R;                         // [experts + 1]; below 0, each its own: nowhere
+    const int copies = 1 << log_copies, dup_copies = 1 << log_dups;
+    Bins bins{lds, lds + ((E + 1) << log_copies), log_copies, static_cast<int>(threadIdx.x) & (copies - 1), log_dups,
+              static_cast<int>(threadIdx.x) & (dup_copies - 1)};
+    int *totals = bins.dups + (R << log_dups);       // [ranks]
+    int *place = totals + R;                         // [experts + 1]
     const int lane = threadIdx.x & (kWave - 1);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.rows.chunk;
     const int lo = static_cast<int>(first);
     const int hi = static_cast<int>(min(first + a.rows.chunk, static_cast<int64_t>(a.rows.tokens)));
-    const int copies = 1 << log_copies, dup_copies = 1 << log_dups;
-    const int copy = threadIdx.x & (copies - 1), dup_copy = threadIdx.x & (dup_copies - 1);
-    if (R) {
-        for (int e = threadIdx.x; e <= E; e += kCountBlock) {
-            const int r = e < E ? a.place[e] : -1;
-            place[e] = static_cast<uint32_t>(r) < static_cast<uint32_t>(R) ? r : -1 - e;
-        }
-    }
+    if (R)
+        for (int e = threadIdx.x; e <= E; e += kCountBlock) place[e] = place_or_none(e < E ? a.place[e] : -1, R, e);
     Segments segments(a.rows, lane);
-    for (int s = segments.first(lo); s < a.rows.segments; ++s) {
-        const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
+    int s = segments.first(lo), at = lo;
+    bool last = false;
+    while (s < a.rows.segments) {
+        const int begin = segments.begin(s), end = segments.end(s), from = max(lo, begin), to = min(hi, end);
         if (begin >= hi) break;
-        if (from >= to) continue;
+        if (end - begin <= a.whole) {
+            // A short segment (or, if none is left out, an empty one).  The next long one begins at row `at` or
+            // behind it; if it does not begin behind row at + kShort, it has that row, or the chunk's last.
+            if (a.whole == 0) {
+                ++s;
+            } else {
+                if (last) break;
+                at = min(at + kShort, hi - 1);
+                last = at == hi - 1;
+                s = max(s + 1, segments.first(at));
+            }
+            continue;
+        }
+        if (from >= to) break;                       // (offsets that do not ascend)
         for (int c = threadIdx.x; c < ((E + 1) << log_copies) + (R << log_dups) + R; c += kCountBlock) lds[c] = 0;
         __syncthreads();
-        for (int64_t u0 = from; u0 < to; u0 += N * kCountBlock) {
-            int idx[N][K];
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if (u0 + n * kCountBlock >= to) break;
-                // (a row that is not there is read as the part's last one, and counts as no expert)
-                const int64_t row = u0 + n * kCountBlock + threadIdx.x;
-                const int32_t *p = a.index + min(row, static_cast<int64_t>(to) - 1) * K;
-                if (K % 4 == 0 && aligned) {
-#pragma unroll
-                    for (int j = 0; j + 3 < K; j += 4) {
-                        const int4 v = *reinterpret_cast<const int4 *>(p + j);
-                        idx[n][j] = v.x;
-                        idx[n][j + 1] = v.y;
-                        idx[n][j + 2] = v.z;
-                        idx[n][j + 3] = v.w;
-                    }
-                } else if (K % 2 == 0 && aligned) {
-#pragma unroll
-                    for (int j = 0; j + 1 < K; j += 2) {
-                        const int2 v = *reinterpret_cast<const int2 *>(p + j);
-                        idx[n][j] = v.x;
-                        idx[n][j + 1] = v.y;
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < K; ++j) idx[n][j] = p[j];
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if (u0 + n * kCountBlock >= to) break;
-                if (u0 + (n + 1) * kCountBlock > to) {                // the last rows of the part
-                    const bool inside = u0 + n * kCountBlock + threadIdx.x < to;
-#pragma unroll
-                    for (int j = 0; j < K; ++j) idx[n][j] = inside ? idx[n][j] : -1;
-                }
-                int rank[K];
-#pragma unroll
-                for (int j = 0; j < K; ++j) {
-                    const uint32_t e = min(static_cast<uint32_t>(idx[n][j]), static_cast<uint32_t>(E));
-                    atomicAdd(&bins[(e << log_copies) + copy], 1);
-                    if (R) rank[j] = place[e];
-                }
-                if (R) {
-#pragma unroll
-                    for (int j = 1; j < K; ++j) {
-                        bool again = false;
-#pragma unroll
-                        for (int i = 0; i < j; ++i) again = again | (rank[i] == rank[j]);
-                        if (again && rank[j] >= 0) atomicAdd(&dups[(rank[j] << log_dups) + dup_copy], 1);
-                    }
-                }
-            }
-        }
+        count_rows<K, kCountBlock>(a, aligned, from, to, R != 0, bins, [&](uint32_t e) { return place[e]; });
         __syncthreads();
         const int M = (a.counts ? E : 0) + R;
         int32_t *part = a.part + (static_cast<int64_t>(blockIdx.x) + s) * M;
         for (int e = threadIdx.x; e < E; e += kCountBlock) {
             int t = 0;
-            for (int c = 0; c < copies; ++c) t += bins[(e << log_copies) + ((c + e) & (copies - 1))];
+            for (int c = 0; c < copies; ++c) t += bins.experts[(e << log_copies) + ((c + e) & (copies - 1))];
             if (a.counts) part[e] = t;
             if (R && place[e] >= 0) atomicAdd(&totals[place[e]], t);
         }
@@ -221,12 +259,58 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_cop
             __syncthreads();
             for (int r = threadIdx.x; r < R; r += kCountBlock) {
                 int t = totals[r];
-                for (int c = 0; c < dup_copies; ++c) t -= dups[(r << log_dups) + ((c + r) & (dup_copies - 1))];
+                for (int c = 0; c < dup_copies; ++c) t -= bins.dups[(r << log_dups) + ((c + r) & (dup_copies - 1))];
                 part[M - R + r] = t;
             }
         }
         __syncthreads();
+        ++s;
+        at = to;
+        last = false;
     }
+}
+
+// A workgroup per segment: the parts of a long one are added, a short one is counted here.
+constexpr int kSegmentBlock = 256;
+
+template <int K>
+__global__ __launch_bounds__(kSegmentBlock) void k_counts_segment(CountArgs a, bool aligned)
+{
+    extern __shared__ int lds[];
+    const int E = a.experts, R = a.rank_tokens ? a.ranks : 0, M = (a.counts ? E : 0) + R;
+    const int64_t s = blockIdx.x;
+    const Parts parts(a.rows, blockIdx.x);
+    int32_t *counts = a.counts + s * E, *tokens = a.rank_tokens + s * R;
+    if (parts.hi - parts.lo > a.whole) {
+        for (int col = threadIdx.x; col < M; col += kSegmentBlock) {
+            int n = 0;
+#pragma unroll 8
+            for (int64_t p = parts.p0; p <= parts.p1; ++p) n += a.part[p * M + col];
+            if (col < M - R) counts[col] = n;
+            else tokens[col - (M - R)] = n;
+        }
+        return;
+    }
+    Bins bins{lds, lds + E + 1, 0, 0, 0, 0};
+    int *totals = bins.dups + R;
+    for (int c = threadIdx.x; c < E + 1 + 2 * R; c += kSegmentBlock) lds[c] = 0;
+    __syncthreads();
+    count_rows<K, kSegmentBlock>(a, aligned, parts.lo, parts.hi, R != 0, bins, [&](uint32_t e) {
+        const int i = static_cast<int>(e);
+        return place_or_none(i < E ? a.place[i] : -1, R, i);
+    });
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kSegmentBlock) {
+        const int t = bins.experts[e];
+        if (a.counts) counts[e] = t;
+        if (R && t != 0) {
+            const int r = place_or_none(a.place[e], R, e);
+            if (r >= 0) atomicAdd(&totals[r], t);
+        }
+    }
+    if (!R) return;
+    __syncthreads();
+    for (int r = threadIdx.x; r < R; r += kSegmentBlock) tokens[r] = totals[r] - bins.dups[r];
 }
 
 // The parts of a segment, as in k_route_finish.
@@ -343,22 +427,35 @@ hipError_t launch_route_backward(const BackwardArgs &a, int32_t dtype, hipStream
 namespace {
 
 template <int K>
-hipError_t counts_of(const CountArgs &a, hipStream_t stream)
+hipError_t counts_of(CountArgs a, hipStream_t stream)
 {
-    // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
-    // workgroups to a CU at the largest sizes; and no more bins than a chunk has slots
-    int log_copies = 5, log_dups = 3;
-    const int64_t slots = std::min<int64_t>(static_cast<int64_t>(a.rows.chunk) * K, 8192);
-    while (log_copies > 0 && static_cast<int64_t>(a.experts) << log_copies > slots) --log_copies;
-    while (log_dups > 0 && static_cast<int64_t>(a.ranks) << log_dups > 2048) --log_dups;
-    const size_t R = a.rank_tokens ? a.ranks : 0, bins = a.experts + 1;
-    const size_t lds = sizeof(int) * ((bins << log_copies) + bins + (R << log_dups) + R);
+    const int E = a.experts, R = a.rank_tokens ? a.ranks : 0, M = (a.counts ? E : 0) + R;
     const bool aligned = reinterpret_cast<uintptr_t>(a.index) % 16 == 0;
-    k_counts<K><<<a.rows.chunks, kCountBlock, lds, stream>>>(a, log_copies, log_dups, aligned);
+    const bool few_segments = many_parts(a.rows);
+    a.whole = few_segments ? 0 : kShort;
+    if (a.rows.tokens > a.whole) {
+        // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
+        // workgroups to a CU at the largest sizes; and no more bins than a chunk has slots
+        int log_copies = 5, log_dups = 3;
+        const int64_t slots = std::min<int64_t>(static_cast<int64_t>(a.rows.chunk) * K, 8192);
+        while (log_copies > 0 && static_cast<int64_t>(E) << log_copies > slots) --log_copies;
+        while (log_dups > 0 && static_cast<int64_t>(R) << log_dups > 2048) --log_dups;
+        const size_t bins = E + 1, ranks = R;
+        const size_t lds = sizeof(int) * ((bins << log_copies) + bins + (ranks << log_dups) + ranks);
+        k_counts<K><<<a.rows.chunks, kCountBlock, lds, stream>>>(a, log_copies, log_dups, aligned);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (few_segments)
+        k_counts_finish<16, 64><<<dim3(a.rows.segments, (M + 15) / 16), 1024, 0, stream>>>(a);
+    else
+        k_counts_segment<K><<<a.rows.segments, kSegmentBlock, sizeof(int) * (E + 1 + 2 * R), stream>>>(a, aligned);
     return hipGetLastError();
 }
 
-hipError_t counts_by_top_k(const CountArgs &a, hipStream_t stream)
+}  // namespace
+
+hipError_t launch_counts(const CountArgs &a, hipStream_t stream)
 {
     switch (a.top_k) {
     case 1: return counts_of<1>(a, stream);
@@ -378,22 +475,6 @@ hipError_t counts_by_top_k(const CountArgs &a, hipStream_t stream)
     case 15: return counts_of<15>(a, stream);
     default: return counts_of<16>(a, stream);
     }
-}
-
-}  // namespace
-
-hipError_t launch_counts(const CountArgs &a, hipStream_t stream)
-{
-    if (a.rows.chunks > 0) {
-        const hipError_t e = counts_by_top_k(a, stream);
-        if (e != hipSuccess) return e;
-    }
-    const int M = (a.counts ? a.experts : 0) + (a.rank_tokens ? a.ranks : 0);
-    if (many_parts(a.rows))
-        k_counts_finish<16, 64><<<dim3(a.rows.segments, (M + 15) / 16), 1024, 0, stream>>>(a);
-    else
-        k_counts_finish<64, 1><<<dim3(a.rows.segments, (M + 63) / 64), 64, 0, stream>>>(a);
-    return hipGetLastError();
 }
 
 hipError_t launch_traffic(int32_t batch, int32_t ranks, const int32_t *rank_tokens, double bytes,

@@ -62,6 +62,7 @@ struct CountArgs {
     const int32_t *index, *place;
     int32_t *counts, *rank_tokens;
     int32_t *part;               // [chunks + segments][experts if counts][ranks if rank_tokens]
+    int32_t whole;               // segments of up to so many rows are not counted in parts
 };
 
 int32_t route_chunk(int32_t tokens, int32_t experts, int32_t most);

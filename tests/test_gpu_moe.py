@@ -465,6 +465,27 @@ def test_counts(B, k, T, E, R, S):
     assert np.array_equal(r, ref[1])
 
 
+@pytest.mark.parametrize("k", [1, 2, 5, 8, 16])
+@pytest.mark.parametrize("lengths", [[1] * 700, [0, 1, 511, 512, 513, 0, 514, 2, 1023, 1024, 1025, 0],
+                                     [1] * 300 + [5000] + [3] * 300 + [700] + [0] * 40, [512], [513], [4097, 1]])
+def test_counts_of_short_and_long_segments(B, k, lengths):
+    """Whole segments that one workgroup counts next to those that are counted in parts, and the lengths
+    between the two; rows before the first segment and behind the last."""
+    rng = np.random.default_rng(len(lengths) + k)
+    E, R = 72, 9
+    seg = 5 + np.r_[0, np.cumsum(lengths)]
+    T = int(seg[-1]) + 7
+    index = np.minimum(rng.zipf(1.5, (T, k)) - 1, 1 << 20).astype(np.int32) % (E + 2) - 1
+    place = rng.integers(-1, R + 1, E)
+    ref = M.counts(index, E, seg, place, R)
+    c, r = gpu_counts(B, index, E, seg, place, R)
+    assert np.array_equal(c, ref[0]) and np.array_equal(r, ref[1])
+    c, _ = gpu_counts(B, index, E, seg)
+    assert np.array_equal(c, ref[0])
+    _, r = gpu_counts(B, index, E, seg, place, R, counts=False)
+    assert np.array_equal(r, ref[1])
+
+
 def test_counts_of_one_hot_expert(B):
     T, k = 200001, 3
     index = np.tile(np.array([5, 9, 2], dtype=np.int32), (T, 1))
