@@ -150,7 +150,7 @@ __device__ __forceinline__ void count_rows(const CountArgs &a, bool aligned, int
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (u0 + n * BLOCK >= to) break;
-            // (a row that is not there is read as the last one, and counts as no expert)
+            // (a row that is not there is read as the last one)
             const int64_t row = u0 + n * BLOCK + threadIdx.x;
             const int32_t *p = a.index + min(row, to - 1) * K;
             if (K % 4 == 0 && aligned) {
@@ -177,11 +177,7 @@ __device__ __forceinline__ void count_rows(const CountArgs &a, bool aligned, int
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (u0 + n * BLOCK >= to) break;
-            if (u0 + (n + 1) * BLOCK > to) {                         // the last rows
-                const bool inside = u0 + n * BLOCK + threadIdx.x < to;
-#pragma unroll
-                for (int j = 0; j < K; ++j) idx[n][j] = inside ? idx[n][j] : -1;
-            }
+            if (u0 + (n + 1) * BLOCK > to && u0 + n * BLOCK + threadIdx.x >= to) continue;   // the last rows
             int rank[K];
 #pragma unroll
             for (int j = 0; j < K; ++j) {
@@ -224,25 +220,11 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_cop
     if (R)
         for (int e = threadIdx.x; e <= E; e += kCountBlock) place[e] = place_or_none(e < E ? a.place[e] : -1, R, e);
     Segments segments(a.rows, lane);
-    int s = segments.first(lo), at = lo;
-    bool last = false;
-    while (s < a.rows.segments) {
-        const int begin = segments.begin(s), end = segments.end(s), from = max(lo, begin), to = min(hi, end);
+    for (int s = segments.longer(segments.first(lo), a.whole, hi); s < a.rows.segments;
+         s = segments.longer(s + 1, a.whole, hi)) {
+        const int begin = segments.begin(s), from = max(lo, begin), to = min(hi, segments.end(s));
         if (begin >= hi) break;
-        if (end - begin <= a.whole) {
-            // A short segment (or, if none is left out, an empty one).  The next long one begins at row `at` or
-            // behind it; if it does not begin behind row at + kShort, it has that row, or the chunk's last.
-            if (a.whole == 0) {
-                ++s;
-            } else {
-                if (last) break;
-                at = min(at + kShort, hi - 1);
-                last = at == hi - 1;
-                s = max(s + 1, segments.first(at));
-            }
-            continue;
-        }
-        if (from >= to) break;                       // (offsets that do not ascend)
+        if (from >= to) continue;
         for (int c = threadIdx.x; c < ((E + 1) << log_copies) + (R << log_dups) + R; c += kCountBlock) lds[c] = 0;
         __syncthreads();
         count_rows<K, kCountBlock>(a, aligned, from, to, R != 0, bins, [&](uint32_t e) { return place[e]; });
@@ -264,9 +246,6 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_cop
             }
         }
         __syncthreads();
-        ++s;
-        at = to;
-        last = false;
     }
 }
 
@@ -282,12 +261,19 @@ __global__ __launch_bounds__(kSegmentBlock) void k_counts_segment(CountArgs a, b
     const Parts parts(a.rows, blockIdx.x);
     int32_t *counts = a.counts + s * E, *tokens = a.rank_tokens + s * R;
     if (parts.hi - parts.lo > a.whole) {
-        for (int col = threadIdx.x; col < M; col += kSegmentBlock) {
-            int n = 0;
-#pragma unroll 8
-            for (int64_t p = parts.p0; p <= parts.p1; ++p) n += a.part[p * M + col];
-            if (col < M - R) counts[col] = n;
-            else tokens[col - (M - R)] = n;
+        for (int c0 = threadIdx.x; c0 < M; c0 += 4 * kSegmentBlock) {    // four columns' reads at a time
+            int n[4] = {0, 0, 0, 0};
+#pragma unroll 2
+            for (int64_t p = parts.p0; p <= parts.p1; ++p) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n[i] += a.part[p * M + min(c0 + i * kSegmentBlock, M - 1)];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int col = c0 + i * kSegmentBlock;
+                if (col < M - R) counts[col] = n[i];
+                else if (col < M) tokens[col - (M - R)] = n[i];
+            }
         }
         return;
     }

@@ -239,6 +239,22 @@ public:
         const unsigned long long hit = __ballot(lane >= 1 && lane <= r.segments && offsets > row);
         return hit == 0 ? r.segments : __ffsll(hit) - 2;
     }
+    // The first segment from s on that has more than `rows` rows (the number of segments, if there is none that
+    // begins before row `end`), 63 at a time.
+    __device__ __forceinline__ int longer(int s, int rows, int end)
+    {
+        if (!r.seg_ptr) return s == 0 && r.tokens <= rows ? r.segments : s;
+        while (s < r.segments) {
+            if (s + 1 - base >= kWave) fetch(s);
+            if (__builtin_amdgcn_readlane(offsets, s - base) >= end) break;
+            const int next = __shfl_down(offsets, 1);
+            const unsigned long long hit = __ballot(lane >= s - base && lane < kWave - 1 && base + lane < r.segments &&
+                                                    next - offsets > rows);
+            if (hit != 0) return base + __ffsll(hit) - 1;
+            s = min(base + kWave - 1, r.segments);
+        }
+        return r.segments;
+    }
     __device__ __forceinline__ int begin(int s) { return r.seg_ptr ? offset(s) : 0; }
     __device__ __forceinline__ int end(int s) { return r.seg_ptr ? offset(s + 1) : r.tokens; }
 
