@@ -83,7 +83,7 @@ int64_t nimble_moe_route_scratch_bytes(int32_t tokens, int32_t experts, int32_t 
     if (tokens < 0 || tokens > NIMBLE_MOE_MAX_TOKENS || experts < 1 || experts > NIMBLE_MOE_MAX_EXPERTS ||
         n_segments < 1 || n_segments > NIMBLE_MOE_MAX_SEGMENTS)
         return -1;
-    const int32_t chunk = moe::route_chunk(tokens, experts, kChunksOfSums);
+    const int32_t chunk = moe::route_chunk(tokens, experts, n_segments, kChunksOfSums);
     return 2 * part_bytes(tokens, chunk, n_segments, experts) + part_bytes(tokens, chunk, n_segments, 1);
 }
 
@@ -105,7 +105,7 @@ nimble_status_t nimble_moe_route(int32_t tokens, int32_t experts, int32_t top_k,
     const bool sums = d_counts || d_routed || d_prob_sum;
     if (sums && !(d_counts && d_routed && d_prob_sum))
         return bad("counts, routed and prob_sum are wanted together or not at all");
-    const int32_t chunk = moe::route_chunk(tokens, experts, sums ? kChunksOfSums : kChunks);
+    const int32_t chunk = moe::route_chunk(tokens, experts, n_segments, sums ? kChunksOfSums : kChunks);
     moe::RouteArgs a{};
     a.rows = rows_of(tokens, chunk, n_segments, d_seg_ptr);
     if (sums) {
@@ -180,7 +180,7 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
         return bad("counts, routed and grad_loss are given together or not at all");
     if (!std::isfinite(alpha)) return bad("alpha must be finite");
     moe::BackwardArgs a{};
-    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, kChunksOfGradient), n_segments, d_seg_ptr);
+    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, n_segments, kChunksOfGradient), n_segments, d_seg_ptr);
     a.experts = experts;
     a.top_k = top_k;
     a.flags = flags;
