@@ -432,8 +432,24 @@ def _moe_logits(t, d_index):
     tokens, experts = t.shape
     if d_index.dim() != 2 or d_index.size(0) != tokens:
         raise ValueError("d_index must be [tokens][top_k]")
+    if tokens > 0x7FFFFFFF or experts > 0x7FFFFFFF:
+        _moe_fits(tokens, experts)
     x, stride = _moe_rows(t, t.dtype, tokens, experts, gpu, "d_logits")
     return gpu, kind, tokens, experts, d_index.size(1), x, stride
+
+
+def _moe_fits(*sizes):
+    """Refuses sizes that ctypes would cut to 32 bits."""
+    for n in sizes:
+        if not -0x80000000 <= n <= 0x7FFFFFFF:
+            raise NimbleError(NIMBLE_ERR_RANGE, f"a size of {n} does not fit 32 bits")
+
+
+def _moe_segments(d_seg_ptr):
+    n = d_seg_ptr.numel() - 1
+    if n > 0x7FFFFFFF:
+        _moe_fits(n)
+    return n
 
 
 def _moe_gpu(t, what):
@@ -489,7 +505,7 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
     bias = keep = seg = counts = routed = prob = scratch = owner = None
     n_seg, nbytes = 1, 0
     if d_seg_ptr is not None:
-        n_seg = d_seg_ptr.numel() - 1
+        n_seg = _moe_segments(d_seg_ptr)
         seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
     if d_bias is not None:
         bias = _moe_ptr(d_bias, f32, experts, gpu, "d_bias")
@@ -517,6 +533,8 @@ def nimble_moe_route(d_logits, d_index, d_weight, *, sigmoid: bool = False, reno
 
 
 def nimble_moe_route_scratch_bytes(tokens: int, experts: int, n_segments: int = 1) -> int:
+    if max(tokens, experts, n_segments) > 0x7FFFFFFF:
+        return -1
     return int(load_library().nimble_moe_route_scratch_bytes(tokens, experts, n_segments))
 
 
@@ -529,6 +547,7 @@ def nimble_moe_balance_loss(d_counts, d_routed, d_prob_sum, top_k: int, alpha: f
     if d_counts.dim() != 2:
         raise ValueError("d_counts must be [segments][experts]")
     n_seg, experts = d_counts.shape
+    _moe_fits(n_seg, experts, top_k)
     args = (n_seg, experts, top_k,
             _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts"),
             _moe_ptr(d_routed, i32, n_seg, gpu, "d_routed"),
@@ -554,7 +573,7 @@ def nimble_moe_route_backward(d_logits, d_index, d_weight, d_grad_logits, *, sig
     keep = seg = grad_weight = counts = routed = grad_loss = None
     n_seg = 1
     if d_seg_ptr is not None:
-        n_seg = d_seg_ptr.numel() - 1
+        n_seg = _moe_segments(d_seg_ptr)
         seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
     if d_keep is not None:
         keep = _moe_ptr(d_keep, _torch.bool if d_keep.dtype is _torch.bool else _torch.uint8, tokens,
@@ -589,10 +608,11 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
     if d_index.dim() != 2:
         raise ValueError("d_index must be [tokens][top_k]")
     tokens, top_k = d_index.shape
+    _moe_fits(tokens, experts)
     seg = place = counts = rank_tokens = None
     n_seg, ranks = 1, 0
     if d_seg_ptr is not None:
-        n_seg = d_seg_ptr.numel() - 1
+        n_seg = _moe_segments(d_seg_ptr)
         seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
     if d_expert_rank is not None:
         place = _moe_ptr(d_expert_rank, i32, experts, gpu, "d_expert_rank")
@@ -615,6 +635,8 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
 
 def nimble_moe_counts_scratch_bytes(tokens: int, top_k: int, experts: int, n_ranks: int = 0,
                                     n_segments: int = 1) -> int:
+    if max(tokens, top_k, experts, n_ranks, n_segments) > 0x7FFFFFFF:
+        return -1
     return int(load_library().nimble_moe_counts_scratch_bytes(tokens, top_k, experts, n_ranks,
                                                               n_segments))
 
@@ -630,6 +652,7 @@ def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traf
     if batch < 1 or d_traffic.numel() % batch:
         raise ValueError("d_traffic must be [batch][commodities]")
     n_comm = d_traffic.numel() // batch
+    _moe_fits(batch, n_comm)
     src = dst = None
     if d_src is not None:
         src = _moe_ptr(d_src, i32, n_comm, gpu, "d_src")

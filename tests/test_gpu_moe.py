@@ -660,3 +660,23 @@ def test_binding_refuses_what_does_not_fit(B):
     with pytest.raises(ValueError):
         B.nimble_moe_traffic(2, torch.zeros((1, 4, 4), dtype=torch.int32, device="cuda:0"), 2.0,
                              torch.zeros((2, 12), dtype=torch.float64, device="cuda:0"))
+
+
+def test_sizes_that_do_not_fit_32_bits(B):
+    """Sizes are not cut to 32 bits on the way: 2^32 + 4 rows are refused, not taken as four."""
+    import torch
+    T, dev = (1 << 32) + 4, "cuda:0"
+    i = torch.empty((T, 1), dtype=torch.int32, device=dev)
+    w = i.view(torch.float32)
+    x = torch.empty((T, 1), dtype=torch.bfloat16, device=dev)
+    count = torch.empty((1, 1), dtype=torch.int32, device=dev)
+    few = torch.empty((4, 1), device=dev)
+    for call in (lambda: B.nimble_moe_route(x, i, w), lambda: B.nimble_moe_route_backward(x, i, w, x),
+                 lambda: B.nimble_moe_counts(i, 1, count),
+                 lambda: B.nimble_moe_route(few, i[:4], w[:4], d_seg_ptr=i.view(-1)[:(1 << 32) + 2]),
+                 lambda: B.nimble_moe_traffic(T, i, 1.0, torch.empty(T, dtype=torch.float64, device=dev)),
+                 lambda: B.nimble_moe_balance_loss(count, count.view(-1), few[0].view(1, 1), (1 << 32) + 1, 1.0,
+                                                   few[0])):
+        with pytest.raises(B.NimbleError) as e:
+            call()
+        assert e.value.status == B.NIMBLE_ERR_RANGE

@@ -199,3 +199,14 @@ def test_binding_refuses_host_tensors():
         B.nimble_moe_route(x.double(), i, w)
     with pytest.raises(TypeError):
         B.nimble_moe_counts(i, 8, i)
+
+
+def test_scratch_of_sizes_that_do_not_fit_32_bits():
+    for at in range(3):
+        sizes = [4, 8, 1]
+        sizes[at] += 1 << 32
+        assert B.nimble_moe_route_scratch_bytes(*sizes) == -1
+    for at in range(5):
+        sizes = [4, 2, 8, 4, 1]
+        sizes[at] += 1 << 32
+        assert B.nimble_moe_counts_scratch_bytes(*sizes) == -1
