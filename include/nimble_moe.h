@@ -77,7 +77,9 @@ enum { NIMBLE_MOE_WAY_BACK = 1u /* the demand of the way back: destination to so
  *   weight   scale * s_e, or with NIMBLE_MOE_RENORM scale * s_e / (sum of s over the row's
  *            chosen experts)
  *   sums     per segment: counts_e = slots that chose e; routed = rows with a choice;
- *            prob_sum_e = sum over these rows of p_e, where p_e = s_e / sum s
+ *            prob_sum_e = sum over these rows of p_e, where p_e = s_e / sum s (up to 64 rows after
+ *            another in binary32, the parts in binary64: adding up costs less than 80 * 2^-24 of
+ *            the sum, whatever the number of rows)
  *
  *   tokens, experts   rows and columns of d_logits; tokens may be 0; 1 <= experts <= 2048
  *   top_k        1 <= top_k <= min(experts, 16)

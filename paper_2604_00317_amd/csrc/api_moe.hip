@@ -16,6 +16,16 @@ namespace moe = nimble::moe;
 
 constexpr int32_t kChunks = 1 << 13, kChunksOfSums = 1 << 9, kChunksOfGradient = 1 << 9;
 
+// Chunks of rows whose probabilities are summed: 512, two workgroups per CU, all of them at work at once, unless that
+// makes a lane add up more than 64 rows in binary32 before the parts are added in binary64: sums of 2^28 equal rows
+// in 512 chunks were off by 1600 roundings (1e-4); in chains of 64 by 7, and of 600 experts by 16 instead of 128.
+constexpr int32_t kChain = 64, kNoSums = NIMBLE_MOE_MAX_TOKENS;
+
+int32_t chunk_of_sums(int32_t tokens, int32_t experts, int32_t n_segments)
+{
+    return moe::route_chunk(tokens, experts, n_segments, kChunksOfSums, kChain);
+}
+
 nimble_status_t bad(const char *what) { return report(NIMBLE_ERR_INVALID, what); }
 nimble_status_t too_large(const char *what) { return report(NIMBLE_ERR_RANGE, what); }
 
@@ -83,7 +93,7 @@ int64_t nimble_moe_route_scratch_bytes(int32_t tokens, int32_t experts, int32_t 
     if (tokens < 0 || tokens > NIMBLE_MOE_MAX_TOKENS || experts < 1 || experts > NIMBLE_MOE_MAX_EXPERTS ||
         n_segments < 1 || n_segments > NIMBLE_MOE_MAX_SEGMENTS)
         return -1;
-    const int32_t chunk = moe::route_chunk(tokens, experts, n_segments, kChunksOfSums);
+    const int32_t chunk = chunk_of_sums(tokens, experts, n_segments);
     return 2 * part_bytes(tokens, chunk, n_segments, experts) + part_bytes(tokens, chunk, n_segments, 1);
 }
 
@@ -105,7 +115,8 @@ nimble_status_t nimble_moe_route(int32_t tokens, int32_t experts, int32_t top_k,
     const bool sums = d_counts || d_routed || d_prob_sum;
     if (sums && !(d_counts && d_routed && d_prob_sum))
         return bad("counts, routed and prob_sum are wanted together or not at all");
-    const int32_t chunk = moe::route_chunk(tokens, experts, n_segments, sums ? kChunksOfSums : kChunks);
+    const int32_t chunk = sums ? chunk_of_sums(tokens, experts, n_segments)
+                               : moe::route_chunk(tokens, experts, n_segments, kChunks, kNoSums);
     moe::RouteArgs a{};
     a.rows = rows_of(tokens, chunk, n_segments, d_seg_ptr);
     if (sums) {
@@ -180,7 +191,8 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
         return bad("counts, routed and grad_loss are given together or not at all");
     if (!std::isfinite(alpha)) return bad("alpha must be finite");
     moe::BackwardArgs a{};
-    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, n_segments, kChunksOfGradient), n_segments, d_seg_ptr);
+    a.rows = rows_of(tokens, moe::route_chunk(tokens, experts, n_segments, kChunksOfGradient, kNoSums), n_segments,
+                     d_seg_ptr);
     a.experts = experts;
     a.top_k = top_k;
     a.flags = flags;

@@ -369,14 +369,15 @@ bool many_parts(const Rows &r) { return r.chunks > 8 * static_cast<int64_t>(r.se
 
 }  // namespace
 
-// Whole passes of a workgroup's rows; with sums no more than 512 chunks, two workgroups per CU, all
-// of them at work at once.  Where segments are shorter than a pass, chunks are too: the parts of a chunk are
-// worked on one after the other.
-int32_t route_chunk(int32_t tokens, int32_t experts, int32_t segments, int32_t most)
+// Whole passes of a workgroup's rows.  Where segments are shorter than a pass, chunks are too: the parts of a
+// chunk are worked on one after the other.
+int32_t route_chunk(int32_t tokens, int32_t experts, int32_t segments, int32_t most, int32_t chain)
 {
-    int32_t pass = kRowWaves * (experts <= 128 ? 8 : experts <= 256 ? 4 : experts <= 512 ? 2 : 1);
+    const int32_t rows = experts <= 256 ? 4 : experts <= 512 ? 2 : 1;    // of a wave, with any top_k
+    int32_t pass = kRowWaves * (experts <= 128 ? 8 : rows);
     if (segments > 1) pass = std::min(pass, round_up(tokens / segments, 8));
-    return round_up((static_cast<int64_t>(tokens) + most - 1) / most, pass);
+    const int64_t even = (static_cast<int64_t>(tokens) + most - 1) / most;
+    return round_up(std::min<int64_t>(even, static_cast<int64_t>(chain) * kRowWaves * rows), pass);
 }
 
 int32_t count_chunk(int32_t tokens, int32_t) { return round_up((static_cast<int64_t>(tokens) + 1023) / 1024, kCountBlock); }

@@ -65,7 +65,9 @@ struct CountArgs {
     int32_t whole;               // segments of up to so many rows are not counted in parts
 };
 
-int32_t route_chunk(int32_t tokens, int32_t experts, int32_t segments, int32_t most);
+// Rows of a chunk: about `most` chunks, but more where a lane would add up the values of more than `chain` rows
+// of one chunk.
+int32_t route_chunk(int32_t tokens, int32_t experts, int32_t segments, int32_t most, int32_t chain);
 int32_t count_chunk(int32_t tokens, int32_t top_k);
 
 hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t stream);

@@ -434,6 +434,31 @@ def test_more_than_2_to_the_31_slots(B):
     assert counts.tolist() == c.tolist() and tokens.tolist() == [[T - 1, T - 1, 0], [1, 1, 0]]
 
 
+@pytest.mark.parametrize("T,E", [((1 << 28) + 5, 8), ((1 << 21) + 3, 600), ((1 << 20) + 1, 256)])
+def test_probability_sums_of_many_rows(B, T, E):
+    """The sum over T equal rows is T times that of one row, but for the roundings of adding up, whose number
+    does not grow with T: 66 rows in a lane at most, 8 lanes' groups in pairs, 8 waves, the result, and
+    that of the one row; the parts' additions in binary64 are below one more.  78 in all."""
+    import torch
+    dev = "cuda:0"
+    rng = np.random.default_rng(E)
+    row = torch.as_tensor(rng.normal(size=(1, E)) * 2).to(dev, torch.bfloat16)
+
+    def sums(x):
+        n = x.shape[0]
+        index = torch.full((n, 1), -2, dtype=torch.int32, device=dev)
+        weight = torch.full((n, 1), math.nan, device=dev)
+        c = torch.zeros((1, E), dtype=torch.int32, device=dev)
+        r = torch.zeros(1, dtype=torch.int32, device=dev)
+        p = torch.full((1, E), math.nan, device=dev)
+        B.nimble_moe_route(x, index, weight, d_counts=c, d_routed=r, d_prob_sum=p)
+        assert r.item() == n and c.sum().item() == n
+        return p.double().cpu().numpy()[0]
+
+    one, many = sums(row), sums(row.expand(T, E).contiguous())
+    assert (np.abs(many - T * one) <= (66 + 3 + 7 + 1 + 1) * U * T * one).all()
+
+
 # ---- counts and demand -----------------------------------------------------------------------
 
 def gpu_counts(B, index, E, seg=None, place=None, ranks=0, counts=True):
