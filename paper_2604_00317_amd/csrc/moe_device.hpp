@@ -167,8 +167,9 @@ __device__ __forceinline__ float sigmoid_of(float x)
     return __builtin_amdgcn_rcpf(1.0f + exp_of(-x));
 }
 
-// exp(x - shift) up to a factor that is the same for all x (2 to the rounding of `at`, shift * log2(e)), in a
-// multiply-add and an exp2.  far(): `at` is so large that the factor may leave the range, or no number.
+// exp(x - shift) and exp(shift - x) up to a factor that is the same for all x (2 to the rounding of `at`,
+// shift * log2(e)), in a multiply-add and an exp2.  far(): `at` is so large that the factor may leave the range,
+// or no number.
 struct Shifted {
     float shift, at;
     __device__ __forceinline__ explicit Shifted(float s) : shift(s), at(s * kLog2E) {}
@@ -178,30 +179,40 @@ struct Shifted {
         return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2E, -at));
     }
     __device__ __forceinline__ float exp(float x) const { return far() ? exp_of(x - shift) : near_exp(x); }
+    // 1 / (exp(shift) + exp(shift - x)), the factor in both terms; `one` is near_one()
+    __device__ __forceinline__ float near_one() const { return __builtin_amdgcn_exp2f(at); }
+    __device__ __forceinline__ float near_sigmoid(float x, float one) const
+    {
+        return __builtin_amdgcn_rcpf(one + __builtin_amdgcn_exp2f(__builtin_fmaf(x, -kLog2E, at)));
+    }
+    __device__ __forceinline__ float sigmoid(float x) const
+    {
+        return far() ? __builtin_amdgcn_rcpf(exp_of(shift) + exp_of(shift - x)) : near_sigmoid(x, near_one());
+    }
 };
 
-// Scores of a row are summed and compared as s(x) exp(-shift).  Softmax: shift is the largest logit.
-// Sigmoid: 0, unless the largest logit is so low that all sigmoids would vanish in 32 bits; it is
-// that logit then, and s(x) = exp(x).
+// Scores of a row are summed and compared as s(x) exp(-shift), so that the largest is about one.  Softmax: shift is
+// the largest logit.  Sigmoid: that logit where it is below 0, else 0 (sigmoids as they are); a row of low logits
+// keeps the ratios of its scores, where sigmoids of logits below -87 would be zeros.
 __device__ __forceinline__ float shift_of(bool sigmoid, float top)
 {
-    return top == -kInf || (sigmoid && top >= -60.0f) ? 0.0f : top;
+    return top == -kInf ? 0.0f : sigmoid ? fminf(top, 0.0f) : top;
 }
 __device__ __forceinline__ float score_of(bool sigmoid, float x, const Shifted &by)
 {
-    const float e = by.exp(x);
-    return sigmoid && by.shift == 0.0f ? sigmoid_of(x) : e;
+    return sigmoid ? by.sigmoid(x) : by.exp(x);
 }
 // All scores of a row's lane; the choice between forms is the wave's.
 template <int V>
 __device__ __forceinline__ void scores_of(bool sigmoid, float (&x)[V], const Shifted &by)
 {
-    if (__ballot(sigmoid ? by.shift != 0.0f : by.far()) != 0) {
+    if (__ballot(by.far()) != 0) {
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] = score_of(sigmoid, x[j], by);
     } else if (sigmoid) {
+        const float one = by.near_one();
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = sigmoid_of(x[j]);
+        for (int j = 0; j < V; ++j) x[j] = by.near_sigmoid(x[j], one);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] = by.near_exp(x[j]);

@@ -266,6 +266,28 @@ def test_rows_far_from_zero(B, offset, dtype):
             assert np.array_equal(served["index"], got["index"])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("E,k", [(24, 4), (200, 8), (1024, 8)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_low_sigmoid_scores(B, dtype, E, k, bias):
+    """Rows whose largest logit is anywhere from 0 to -72, the others up to 90 lower: probabilities and
+    divided weights depend on differences alone, far below the logits whose sigmoids are numbers."""
+    import torch
+    rng = np.random.default_rng(E)
+    T = 72
+    x = -rng.uniform(0, 90, (T, E)) - np.arange(T)[:, None]
+    d = torch.as_tensor(x).to("cuda:0", getattr(torch, dtype))
+    x = d.float().cpu().numpy()
+    b = rng.uniform(-60, 60, E).astype(np.float32) if bias else None
+    for renorm in (False, True):
+        kw = dict(sigmoid=True, renorm=renorm, bias=b, grad_weight=rng.normal(size=(T, k)).astype(np.float32),
+                  grad_loss=np.ones(1, dtype=np.float32), alpha=0.5)
+        got = run(B, d, k, backward=True, **kw)
+        check(got, x, k, dtype, **kw)
+        served = run(B, d, k, sums=False, sigmoid=True, renorm=renorm, bias=b)
+        check(served, x, k, dtype, sigmoid=True, renorm=renorm, bias=b)
+
+
 def test_a_bias_that_excludes_and_one_that_forces(B):
     import torch
     rng = np.random.default_rng(9)
