@@ -133,7 +133,8 @@ nimble_status_t nimble_moe_balance_loss(int32_t n_segments, int32_t experts, int
  * Rows left out by d_keep and rows without a choice get zeros.
  *
  *   d_index, d_weight   what nimble_moe_route gave for the same logits, flags, scale, d_keep and
- *                  segments (indices outside 0 .. experts-1 are empty slots)
+ *                  segments (indices outside 0 .. experts-1 are empty slots; an index that a row holds
+ *                  more than once adds up, in the order of the slots)
  *   d_grad_weight  float [tokens][top_k], or NULL for zeros
  *   d_counts, d_routed, d_grad_loss   [n_segments][experts], [n_segments], float [n_segments]:
  *                  all three, or all NULL: no loss

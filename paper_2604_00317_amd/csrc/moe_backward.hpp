@@ -95,7 +95,8 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             const float wg = there ? w * gw : 0.0f;
             const float all = group_sum<kSlots>(wg);
             const float slope = w * ((there ? gw : 0.0f) - (renorm ? all * per_scale : 0.0f));
-            if (index >= 0 && inside) atomicAdd(&mine[index], slope);
+            float before = 0.0f;
+            if (index >= 0 && inside) before = atomicAdd(&mine[index], slope);
             float x[V], sum = 0.0f, rest = 0.0f, r[V];
             raw.end_at(a.experts, l, shape);
             raw.values(x);
@@ -124,6 +125,16 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             rest = group_sum<L>(rest) * inv;
             // sums over the slots are in the lanes that have them
             if (!sigmoid && !renorm) rest = rest + __shfl(all, lane & ~(L - 1));
+            // LDS adds slots of the same expert (a router's choice has none) in any order; where a column got more than
+            // one, all are added again in the order of the slots.  (0 to 3 % of the kernel's time)
+            if (__ballot(before != 0.0f) != 0) {
+                float total = 0.0f;
+                for (int i = 0; i < a.top_k; ++i) {
+                    const float other = __shfl(slope, (lane & ~(L - 1)) + i);
+                    total = __shfl(index, (lane & ~(L - 1)) + i) == index ? total + other : total;
+                }
+                if (index >= 0 && inside) mine[index] = total;
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int q = 0; q < V / kRun; ++q) {

@@ -412,6 +412,30 @@ def test_indices_of_another_router(B):
     assert (np.abs(out.cpu().numpy() - dx) <= 3 * rel(x)[:, None] * mag + U * np.abs(dx)).all()
 
 
+@pytest.mark.parametrize("E,k", [(32, 5), (100, 8), (100, 16), (256, 16), (500, 9), (1024, 16)])
+def test_repeated_indices_add_up_in_the_order_of_the_slots(B, E, k):
+    """Slots of masked experts (probability 0), weights of one: their columns hold the sum of the weights'
+    gradients in binary32, one slot after the other, of numbers that add up differently in other orders."""
+    import torch
+    rng = np.random.default_rng(E + k)
+    T = 50
+    x = rng.normal(size=(T, E)).astype(np.float32)
+    x[:, 1:4] = -np.inf
+    idx = rng.integers(1, 4, (T, k)).astype(np.int32)
+    idx[0], idx[1, k // 2:], idx[2, 1::2] = 2, -1, E
+    idx[3::7] = np.argsort(rng.random((len(idx[3::7]), E)))[:, :k]          # rows without a repeated one
+    g = (rng.normal(size=(T, k)) * 2.0 ** rng.integers(-12, 12, (T, k))).astype(np.float32)
+    d = lambda a: torch.as_tensor(a).to("cuda:0")   # noqa: E731
+    out = torch.full((T, E), math.nan, device="cuda:0")
+    B.nimble_moe_route_backward(d(x), d(idx), torch.ones((T, k), device="cuda:0"), out, renorm=False, d_grad_weight=d(g))
+    want = np.zeros((T, E), dtype=np.float32)
+    for t in range(T):
+        for j in range(k):
+            if 1 <= idx[t, j] < 4:
+                want[t, idx[t, j]] = np.float32(want[t, idx[t, j]] + g[t, j])
+    assert np.array_equal(out.cpu().numpy()[:, 1:4], want[:, 1:4])
+
+
 def test_offsets_beyond_32_bits(B):
     """Rows 2^31 + 64 elements apart."""
     import torch
