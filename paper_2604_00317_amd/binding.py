@@ -432,10 +432,11 @@ def _moe_logits(t, d_index):
     tokens, experts = t.shape
     if d_index.dim() != 2 or d_index.size(0) != tokens:
         raise ValueError("d_index must be [tokens][top_k]")
-    if tokens > 0x7FFFFFFF or experts > 0x7FFFFFFF:
-        _moe_fits(tokens, experts)
+    top_k = d_index.size(1)
+    if tokens > 0x7FFFFFFF or experts > 0x7FFFFFFF or top_k > 0x7FFFFFFF:
+        _moe_fits(tokens, experts, top_k)
     x, stride = _moe_rows(t, t.dtype, tokens, experts, gpu, "d_logits")
-    return gpu, kind, tokens, experts, d_index.size(1), x, stride
+    return gpu, kind, tokens, experts, top_k, x, stride
 
 
 def _moe_fits(*sizes):
@@ -608,9 +609,11 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
     if d_index.dim() != 2:
         raise ValueError("d_index must be [tokens][top_k]")
     tokens, top_k = d_index.shape
-    _moe_fits(tokens, experts)
     seg = place = counts = rank_tokens = None
     n_seg, ranks = 1, 0
+    if d_rank_tokens is not None:
+        ranks = d_rank_tokens.size(-1)
+    _moe_fits(tokens, top_k, experts, ranks)
     if d_seg_ptr is not None:
         n_seg = _moe_segments(d_seg_ptr)
         seg = _moe_ptr(d_seg_ptr, i32, n_seg + 1, gpu, "d_seg_ptr")
@@ -619,7 +622,6 @@ def nimble_moe_counts(d_index, experts: int, d_counts=None, *, d_expert_rank=Non
     if d_counts is not None:
         counts = _moe_ptr(d_counts, i32, n_seg * experts, gpu, "d_counts")
     if d_rank_tokens is not None:
-        ranks = d_rank_tokens.size(-1)
         rank_tokens = _moe_ptr(d_rank_tokens, i32, n_seg * ranks, gpu, "d_rank_tokens")
     scratch, nbytes, owner = _moe_scratch(
         d_scratch, lib.nimble_moe_counts_scratch_bytes(tokens, top_k, experts, ranks, n_seg), gpu,
@@ -652,7 +654,7 @@ def nimble_moe_traffic(batch: int, d_rank_tokens, bytes_per_token: float, d_traf
     if batch < 1 or d_traffic.numel() % batch:
         raise ValueError("d_traffic must be [batch][commodities]")
     n_comm = d_traffic.numel() // batch
-    _moe_fits(batch, n_comm)
+    _moe_fits(batch, ranks, n_comm)
     src = dst = None
     if d_src is not None:
         src = _moe_ptr(d_src, i32, n_comm, gpu, "d_src")

@@ -751,3 +751,21 @@ def test_sizes_that_do_not_fit_32_bits(B):
         with pytest.raises(B.NimbleError) as e:
             call()
         assert e.value.status == B.NIMBLE_ERR_RANGE
+
+
+def test_slots_and_gpus_that_do_not_fit_32_bits(B):
+    """Nor are slots per row and GPUs: 2^32 + 2 of them are refused, not taken as two."""
+    import torch
+    dev, n = "cuda:0", (1 << 32) + 2
+    i = torch.empty((1, n), dtype=torch.int32, device=dev)
+    w, x = i.view(torch.float32), torch.zeros((1, 8), device=dev)
+    few = torch.zeros((1, 2), dtype=torch.int32, device=dev)
+    place, count = torch.zeros(8, dtype=torch.int32, device=dev), torch.zeros((1, 8), dtype=torch.int32, device=dev)
+    for call in (lambda: B.nimble_moe_route(x, i, w),
+                 lambda: B.nimble_moe_route_backward(x, i, w, torch.zeros_like(x)),
+                 lambda: B.nimble_moe_counts(i, 8, count),
+                 lambda: B.nimble_moe_counts(few, 8, d_expert_rank=place, d_rank_tokens=i),
+                 lambda: B.nimble_moe_traffic(1, i, 1.0, torch.empty(2, dtype=torch.float64, device=dev))):
+        with pytest.raises(B.NimbleError) as e:
+            call()
+        assert e.value.status == B.NIMBLE_ERR_RANGE
