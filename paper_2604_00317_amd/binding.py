@@ -52,13 +52,17 @@ EXPORTS = [
 _lib = None
 _torch = None               # the module, once the library is loaded
 _MOE_KINDS = {}             # element types of logits
-_current_gpu = _raw_stream = None   # torch's own, without its checks
+_current_gpu = _raw_stream = None   # torch's own, without its checks where it has such
 
 
 class NimbleError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"nimble status {status}: {message}")
         self.status = status
+
+
+def _public_stream(gpu: int) -> int:
+    return _torch.cuda.current_stream(gpu).cuda_stream
 
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
@@ -77,8 +81,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     # round, torch finds a runtime it was not built for and reports no GPU).
     import torch
     _torch = torch
-    _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
-    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_stream)
     _MOE_KINDS.update({torch.float32: NIMBLE_F32, torch.float16: NIMBLE_F16,
                        torch.bfloat16: NIMBLE_BF16})
     lib = ctypes.CDLL(LIB_PATH)

@@ -769,3 +769,21 @@ def test_slots_and_gpus_that_do_not_fit_32_bits(B):
         with pytest.raises(B.NimbleError) as e:
             call()
         assert e.value.status == B.NIMBLE_ERR_RANGE
+
+
+def test_calls_by_torchs_public_device_and_stream(B, monkeypatch):
+    """The slower way of a torch without bare functions: same stream, same results."""
+    import torch
+    rng = np.random.default_rng(3)
+    x = logits(rng, 300, 64, "float32")
+    ref = run(B, x, 4)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        bare = B._current_gpu(), B._raw_stream(0)
+    monkeypatch.setattr(B, "_current_gpu", torch.cuda.current_device)
+    monkeypatch.setattr(B, "_raw_stream", B._public_stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        assert (B._current_gpu(), B._raw_stream(0)) == bare == (0, s.cuda_stream)
+        got = run(B, x, 4)
+    assert all(np.array_equal(got[n], ref[n]) for n in ref)

@@ -210,3 +210,18 @@ def test_scratch_of_sizes_that_do_not_fit_32_bits():
         sizes = [4, 2, 8, 4, 1]
         sizes[at] += 1 << 32
         assert B.nimble_moe_counts_scratch_bytes(*sizes) == -1
+
+
+def test_without_torchs_bare_device_and_stream(monkeypatch):
+    """Where torch lacks the bare functions, the public ones are asked."""
+    import torch
+    from types import SimpleNamespace
+    B.load_library()
+    for name in ("_lib", "_current_gpu", "_raw_stream"):
+        monkeypatch.setattr(B, name, None)
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 5)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda gpu: SimpleNamespace(cuda_stream=1000 + gpu))
+    B.load_library()
+    assert B._current_gpu() == 5 and B._raw_stream(7) == 1007
