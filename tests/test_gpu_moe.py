@@ -787,3 +787,90 @@ def test_calls_by_torchs_public_device_and_stream(B, monkeypatch):
         assert (B._current_gpu(), B._raw_stream(0)) == bare == (0, s.cuda_stream)
         got = run(B, x, 4)
     assert all(np.array_equal(got[n], ref[n]) for n in ref)
+
+
+# ---- forms that the tests above leave out ------------------------------------------------------
+
+@pytest.mark.parametrize("k", [1, 2, 3, 5, 9, 15, 16])
+@pytest.mark.parametrize("E", [16, 100, 700])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_ties_of_16_bit_logits(B, k, E, dtype):
+    """Five values that both types hold, without a bias and with one of as many: nearly every choice is a tie."""
+    import torch
+    rng = np.random.default_rng(k * E)
+    v = np.array([-1.0, -0.0, 0.0, 0.5, 2.0], dtype=np.float32)
+    x = v[rng.integers(0, 5, (33, E))]
+    x[5] = -0.0
+    x[6] = 1.0
+    d = torch.as_tensor(x).to("cuda:0", getattr(torch, dtype))
+    for bias in (None, v[rng.integers(0, 5, E)]):
+        for sums in (False, True):
+            got = run(B, d, k, bias=bias, sums=sums)
+            check(got, x, k, dtype, bias=bias)
+
+
+@pytest.mark.parametrize("E,k", [(16, 9), (16, 16), (60, 12), (100, 9), (128, 16), (130, 10), (256, 16), (300, 11),
+                                 (700, 16), (2048, 13)])
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_more_than_eight_slots(B, dtype, E, k):
+    """The gradient over nine to sixteen slots; rows with fewer experts than slots, or none, among them."""
+    import torch
+    rng = np.random.default_rng(E * k)
+    T = 37
+    x = rng.normal(size=(T, E)) * 2
+    x[3, 2:] = -np.inf
+    x[4, :E - k + 1] = -np.inf
+    x[5] = -np.inf
+    d = torch.as_tensor(x).to("cuda:0", getattr(torch, dtype))
+    form = dict(keep=rng.random(T) < 0.8, seg=[0, 11, 11, T - 2], alpha=0.3, scale=2.5,
+                grad_weight=rng.normal(size=(T, k)).astype(np.float32), grad_loss=rng.normal(size=3).astype(np.float32))
+    for sigmoid in (False, True):
+        for renorm in (False, True):
+            kw = dict(form, sigmoid=sigmoid, renorm=renorm)
+            got = run(B, d, k, backward=True, **kw)
+            check(got, d.float().cpu().numpy(), k, dtype, **kw)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+@pytest.mark.parametrize("E", [5, 32, 64, 128, 160, 256, 500, 1024, 2048])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_few_slots_of_16_bit_logits(B, dtype, E, k):
+    rng = np.random.default_rng(E * k)
+    x = logits(rng, 40, E, dtype)
+    for sums in (False, True):
+        for renorm in (False, True):
+            got = run(B, x, k, sums=sums, renorm=renorm)
+            check(got, x.float().cpu().numpy(), k, dtype, renorm=renorm)
+
+
+@pytest.mark.parametrize("k", [1, 8, 16])
+@pytest.mark.parametrize("T,S", [(5000, 1), (3000, 40), (9000, 3)])
+def test_counts_of_the_most_experts_and_gpus(B, k, T, S):
+    """2048 experts on 4096 GPUs, the most bins in LDS, forty of them on the last GPU; segments in parts and whole."""
+    rng = np.random.default_rng(k + T)
+    E, R = 2048, 4096
+    index = rng.integers(-1, E + 1, (T, k)).astype(np.int32)
+    place = rng.integers(-1, R + 1, E)
+    place[:40] = R - 1
+    seg = np.sort(rng.integers(0, T + 1, S + 1))
+    ref = M.counts(index, E, seg, place, R)
+    c, r = gpu_counts(B, index, E, seg, place, R)
+    assert np.array_equal(c, ref[0]) and np.array_equal(r, ref[1])
+    _, r = gpu_counts(B, index, E, seg, place, R, counts=False)
+    assert np.array_equal(r, ref[1])
+
+
+@pytest.mark.parametrize("S", [2, 128, 700])
+def test_one_segment_holds_nearly_all_rows(B, S):
+    """The parts of a long segment among short ones are all added, by the calls for few segments and for many."""
+    rng = np.random.default_rng(S)
+    E, k, T = 64, 4, 30000
+    short = np.sort(rng.integers(0, 500, S - 1))
+    seg = np.r_[0, short[:S // 2], T - 500 + short[S // 2:], T]
+    x = logits(rng, T, E, "bfloat16")
+    got = run(B, x, k, seg=seg, alpha=0.1)
+    check(got, x.float().cpu().numpy(), k, "bfloat16", seg=seg, alpha=0.1)
+    place = np.arange(E) % 6
+    c, r = gpu_counts(B, got["index"], E, seg, place, 6)
+    ref = M.counts(got["index"], E, seg, place, 6)
+    assert np.array_equal(c, got["counts"]) and np.array_equal(c, ref[0]) and np.array_equal(r, ref[1])
