@@ -105,7 +105,10 @@ nimble_status_t nimble_moe_route(int32_t tokens, int32_t experts, int32_t top_k,
                                  float *d_prob_sum, void *d_scratch, int64_t scratch_bytes,
                                  void *hip_stream);
 
-/* Scratch bytes of nimble_moe_route with sums; -1 for sizes it refuses. */
+/*
+ * Scratch bytes of nimble_moe_route with sums; -1 for sizes it refuses.  They do not rise with every
+ * size: a call with fewer rows may need more, so memory for calls of several sizes is the most of theirs.
+ */
 int64_t nimble_moe_route_scratch_bytes(int32_t tokens, int32_t experts, int32_t n_segments);
 
 /*
@@ -159,7 +162,9 @@ nimble_status_t nimble_moe_route_backward(int32_t tokens, int32_t experts, int32
  *   d_expert_rank  int32 [experts]: the GPU an expert lives on; entries outside
  *                  0 .. n_ranks-1 live nowhere
  *   d_rank_tokens  int32 [n_segments][n_ranks] out or NULL: rows with at least one expert on
- *                  that GPU (a token goes to a GPU once, however many of its experts are there)
+ *                  that GPU: a token goes to a GPU once, however many of its experts are there.
+ *                  (An All-to-Allv that sends every slot carries up to top_k times as much: the sums
+ *                  of d_counts over the experts of a GPU, which no call here makes.)
  * At least one of the outputs; n_ranks >= 1 and d_expert_rank with d_rank_tokens.
  */
 nimble_status_t nimble_moe_counts(int32_t tokens, int32_t top_k, const int32_t *d_index,
@@ -168,7 +173,7 @@ nimble_status_t nimble_moe_counts(int32_t tokens, int32_t top_k, const int32_t *
                                   int32_t *d_counts, int32_t *d_rank_tokens, void *d_scratch,
                                   int64_t scratch_bytes, void *hip_stream);
 
-/* Scratch bytes of nimble_moe_counts; -1 for sizes it refuses.  n_ranks 0: no rank tokens. */
+/* Scratch bytes of nimble_moe_counts, as above; -1 for sizes it refuses.  n_ranks 0: no rank tokens. */
 int64_t nimble_moe_counts_scratch_bytes(int32_t tokens, int32_t top_k, int32_t experts,
                                         int32_t n_ranks, int32_t n_segments);
 

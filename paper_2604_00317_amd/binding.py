@@ -900,7 +900,10 @@ def plan_routed(topo: Topo, d_logits, d_seg_ptr, d_expert_rank, top_k: int, byte
                 d_dst=None):
     """Convenience wrapper of the routing operators and the planner: logits [tokens][experts] of all
     source GPUs (one segment each, d_seg_ptr [ranks + 1]) in; a dict of device tensors out: the
-    choice (index, weight), rank_tokens, the demand (traffic), splits and lambda of its plan.  Only
+    choice (index, weight; weights divided by their sum), rank_tokens, the demand (traffic), splits
+    and lambda of its plan.  A token goes to a GPU once, however many of its experts are there:
+    workloads.moe_traffic, which counts every slot, gives up to top_k times as many bytes.  One
+    layer, every row routed; other forms are the calls below, one by one.  Only
     enqueues work on the current stream.  d_src and d_dst: the GPUs of the commodities, where they
     are not all ordered pairs in row-major order."""
     import torch

@@ -37,7 +37,7 @@ struct Parts {
 // Parts are added by the threads of a workgroup in COLS columns and 1024 / COLS (or one) rows: every row
 // adds each rows-th part, and the first one the rows' sums in order.  What bounds these kernels is the time
 // of a few dependent reads, so many parts (of few segments) take many rows and few columns, and few parts
-// one row and a workgroup of one wave: 3.4 to 5.2 us for 32 to 512 parts of 64 to 1024 columns.
+// one row and a workgroup of one wave: 3.4 to 5.9 us for 32 to 512 parts of 64 to 1024 columns.
 template <int COLS, int ROWS>
 __global__ __launch_bounds__(COLS *ROWS) void k_route_finish(RouteArgs a)
 {
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(COLS *ROWS) void k_route_finish(RouteArgs a)
 // ---- loss ------------------------------------------------------------------------------------
 
 // A workgroup per segment, of up to 1024 threads: all reads are under way at once (1.6 us for one segment of 64
-// experts, 4.3 for one of 1024; no more than a launch and the reads' latency).
+// experts, 3.8 for one of 1024; no more than a launch and the reads' latency).
 __global__ __launch_bounds__(1024) void k_balance_loss(int experts, double unit, const int32_t *counts,
                                                        const int32_t *routed, const float *prob_sum,
                                                        float *loss)
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kCountBlock) void k_counts(CountArgs a, int log_cop
     }
 }
 
-// A workgroup per segment: the parts of a long one are added, a short one is counted here (2.5 to 5.2 us).
+// A workgroup per segment: the parts of a long one are added, a short one is counted here (3.9 to 5.2 us).
 constexpr int kSegmentBlock = 256;
 
 template <int K>
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(COLS *ROWS) void k_counts_finish(CountArgs a)
     else a.rank_tokens[s * a.ranks + col - E] = n;
 }
 
-// A thread per commodity; 2.0 to 4.7 us, a launch and two dependent reads.
+// A thread per commodity; 1.9 to 4.8 us, a launch and two dependent reads.
 __global__ __launch_bounds__(256) void k_traffic(int64_t total, int ranks, const int32_t *tokens,
                                                  double bytes, int n_comm, const int32_t *src,
                                                  const int32_t *dst, bool way_back, double *traffic)
@@ -426,8 +426,9 @@ hipError_t counts_of(CountArgs a, hipStream_t stream)
     const bool few_segments = many_parts(a.rows);
     a.whole = few_segments ? 0 : kShort;
     if (a.rows.tokens > a.whole) {
-        // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits): three
-        // workgroups to a CU at the largest sizes; and no more bins than a chunk has slots
+        // as many copies as 32 KiB hold, up to 32 (and 8 KiB, up to 8, of the bins of double visits), and no more
+        // bins than a chunk has slots: 47 KB for 1024 experts on 512 GPUs, three workgroups to a CU; 74 KB, two,
+        // for 2048 on 4096
         int log_copies = 5, log_dups = 3;
         const int64_t slots = std::min<int64_t>(static_cast<int64_t>(a.rows.chunk) * K, 8192);
         while (log_copies > 0 && static_cast<int64_t>(E) << log_copies > slots) --log_copies;

@@ -1,8 +1,8 @@
 // Gradient of the logits (include/nimble_moe.h).  Rows lie in lanes as in moe_route.hpp.  One pass over the
 // logits: probabilities are made again (a stored sum would save 4 bytes of 2 KB, and lose accuracy for
 // large logits), the choice's part comes through LDS, a float per column of every row at work.  Reading
-// and writing bound it: 16384 rows of 1024 in f32 24 us (5.6 TB/s), 1 M rows of 256 in bf16 255 us (4.6 TB/s; the
-// vector units are busy for 60 % of it).
+// and writing bound it: 16384 rows of 1024 in f32 25 us (5.4 TB/s), 1 M rows of 256 in bf16 263 us (4.5 TB/s; the
+// vector units are busy for 62 % of the cycles in which waves are there).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kRowWaves *kWave) void k_route_backward(BackwardArg
             // sums over the slots are in the lanes that have them
             if (!sigmoid && !renorm) rest = rest + __shfl(all, lane & ~(L - 1));
             // LDS adds slots of the same expert (a router's choice has none) in any order; where a column got more than
-            // one, all are added again in the order of the slots.  (0 to 3 % of the kernel's time)
+            // one, all are added again in the order of the slots.  (Looking costs 0 to 3 % of the kernel's time, 5 with 64 experts, top-8, sigmoids.)
             if (__ballot(before != 0.0f) != 0) {
                 float total = 0.0f;
                 for (int i = 0; i < a.top_k; ++i) {
